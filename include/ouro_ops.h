@@ -174,6 +174,33 @@ int ouro_op_embed_fwd(void* stream, int dtype, const int32_t* tok, const void* V
 /* dVi (fp32 [vocab,d], overwritten) = scatter-add of scale*dh rows (Eq. 7, left). */
 int ouro_op_embed_bwd(void* stream, int dtype, const int32_t* tok, const void* dh, float* dVi,
                       int N, int d, int vocab, float scale);
+/* The same gradient with sums in an order that the ids alone determine: dV[v,:] = scale * sum of the rows dh[n,:] with
+ * tok[n] = v, or with accumulate != 0 dV[v,:] += that (a tied matrix that already holds its other gradient: only the rows of
+ * ids that occur are read and written).  dh [N, lddh] of type T, dV fp32 [vocab, ldv]; lddh, ldv >= d, any alignment of an
+ * element.  Ids outside [0, vocab) take no part.  N = 0 is allowed (tok, dh are not used then); N <= 2^30.  One launch,
+ * no workspace; equal calls give equal bits. */
+int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv, int N,
+                             int d, int vocab, float scale, int accumulate);
+/* Gated linear recurrence over B streams of T steps and D channels: f = sigmoid(z), h_t = f_t h_{t-1} + (1 - f_t) x_t.
+ * z, x, h: rows b*T+t of type T (ld* in elements, >= D, any alignment of an element).  h0 fp32 [B, D], the state that enters
+ * step 0 (NULL: zero); hT fp32 [B, D], the state behind the last step (may be NULL).  States are fp32 throughout.  z = +infinity
+ * gives f = 1 (the state is kept), -infinity f = 0.  T = 1 is the form for single tokens; h0 and hT may then, as always, be one buffer.
+ * lens: int32 [B], device, or NULL: stream b has lens[b] steps (taken as 0 below 0, as T above T); rows behind them are not
+ * read, h is zero there, and the state stays what it is.
+ * states: fp32 [B, ceil(T / OURO_RECURRENCE_STRIDE), D] or NULL: the state that enters every OURO_RECURRENCE_STRIDE-th
+ * step, which is what the backward call needs.
+ * scratch: fp32, ouro_op_recurrence_scratch() floats (NULL where that is 0); a few long streams are cut into segments.
+ * No output may overlap an input, but for h0 and hT.  T <= 2^30. */
+enum { OURO_RECURRENCE_STRIDE = 64 };
+int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
+                           const float* h0, const int32_t* lens, void* h, int ldh, float* hT, float* states, float* scratch);
+/* Backward of the above from z, x, states and lens as they were: dh rows of type T, dhT fp32 [B, D] the gradient of hT (NULL:
+ * zero).  dz, dx (type T) and dh0 (fp32 [B, D], may be NULL) are overwritten; rows behind a stream's length are zero in dz and dx,
+ * and dh is not read there.  dhT and dh0 may be one buffer. */
+int ouro_op_recurrence_bwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
+                           const float* states, const int32_t* lens, const void* dh, int lddh, const float* dhT, void* dz,
+                           int lddz, void* dx, int lddx, float* dh0, float* scratch);
+size_t ouro_op_recurrence_scratch(int B, int T, int D);
 /* Rows of logits [N, ld] (type T): lse[n]; rowloss[n] = lse - logit[tgt]; G (T, [N, ldg]) =
  * (softmax - onehot)/N, which may be the logits buffer itself (in place); *loss =
  * mean(rowloss) (Eq. 4).  flag bit 1: target out of range. */

@@ -119,6 +119,10 @@ def lib():
         "ouro_op_colsum": (i32, [vp, i32, vp, i32, vp, i32, i32]),
         "ouro_op_embed_fwd": (i32, [vp, i32, vp, vp, vp, vp, i32, i32, i32, i32, f32, vp]),
         "ouro_op_embed_bwd": (i32, [vp, i32, vp, vp, vp, i32, i32, i32, f32]),
+        "ouro_op_embed_bwd_sorted": (i32, [vp, i32, vp, vp, i32, vp, i32, i32, i32, i32, f32, i32]),
+        "ouro_op_recurrence_fwd": (i32, [vp, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp]),
+        "ouro_op_recurrence_bwd": (i32, [vp, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32, vp, vp]),
+        "ouro_op_recurrence_scratch": (sz, [i32, i32, i32]),
         "ouro_op_softmax_ce": (i32, [vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32, i32, vp]),
         "ouro_op_update": (i32, [vp, vp, vp, vp, vp, vp, f32, vp, f32, sz, i32, f32, f32, f32, f32, i64]),
         "ouro_op_update_groups": (i32, [vp, i32, P(vp), P(vp), P(vp), P(vp), P(vp), P(vp), P(f32), P(vp), P(f32), P(sz), P(vp), P(i32), P(i32), i32,

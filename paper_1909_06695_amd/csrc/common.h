@@ -193,6 +193,30 @@ int set_error(int code, const char* msg);
 hipError_t launch_attn_fwd(hipStream_t s, int dtype, const AttnDesc& a, int force_generic);
 hipError_t launch_attn_bwd(hipStream_t s, int dtype, const AttnDesc& a, int force_generic);
 
+// --------------------------------------------------------------------------- recurrence
+// h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(z), per stream and channel; rows b*T + t of type T, states fp32 [B, D].
+// Steps t >= lens[b] (null: none) are not taken, their rows not read and written as zero.  states [B, ceil(T / stride), D]: the
+// state that enters every RECURRENCE_STRIDE-th step (forward: written unless null; backward: read).  dz null: forward.
+constexpr int RECURRENCE_STRIDE = 64;
+struct RecurrenceDesc {
+  int B, T, D;
+  const void* z; int ldz;
+  const void* x; int ldx;
+  const int32_t* lens;
+  float* states;
+  float* scratch;                  // recurrence_scratch_floats() elements
+  const float* h0;                 // forward; null: zero
+  void* h; int ldh;
+  float* hT;                       // or null
+  const void* dh; int lddh;        // backward
+  const float* dhT;                // or null: zero
+  void* dz; int lddz;
+  void* dx; int lddx;
+  float* dh0;                      // or null
+};
+size_t recurrence_scratch_floats(int B, int T, int D);
+hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r);
+
 // -------------------------------------------------------------------- row-wise kernels
 // y = LN(x) * g + b over rows of d elements (biased variance, eps 1e-5); saves mean, rstd.
 // Rows are d wide; the statistics run over the first dn columns (dn = 0: all d).  With dn < d the
@@ -236,6 +260,10 @@ hipError_t launch_embed_fwd(hipStream_t s, int dtype, const int32_t* tok, const 
 // dVi[tok[n],:] += scale * dh[n,:]   (fp32 atomics; caller zeroes dVi); dtype: type of dh (1 bf16, else fp32)
 hipError_t launch_embed_bwd(hipStream_t s, int dtype, const int32_t* tok, const void* dh, float* dVi,
                             int N, int d, int vocab, float scale, const DropDesc* drop = nullptr);
+// dV[v, :] (=, with accumulate +=) scale * sum of dh[n, :] over tok[n] = v, in an order that the ids determine; dtype: type of dh;
+// leading dimensions in elements.  Ids outside [0, vocab) take no part.
+hipError_t launch_embed_bwd_sorted(hipStream_t s, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv,
+                                   int N, int d, int vocab, float scale, int accumulate);
 // One matrix of a parameter blob to be kept transposed as well: bf16 [rows, cols] at element offset
 // off of src -> [cols, rows] with leading dimension ld_out at the same offset of dst.  tile0 is the
 // running count of 64x64 tiles before this matrix (the launch covers all matrices of a table).

@@ -283,6 +283,59 @@ extern "C" int ouro_op_embed_bwd(void* stream, int dtype, const int32_t* tok, co
   return rc_of(launch_embed_bwd(s, dtype, tok, dh, dVi, N, d, vocab, scale));
 }
 
+static int refuse(const char* op, const char* why) {
+  char msg[200];
+  snprintf(msg, sizeof msg, "%s: %s", op, why);
+  return set_error(OURO_E_ARG, msg);
+}
+constexpr int ROWS_MAX = 1 << 30;                                 // rows and steps that the kernels count in 32 bits, with room for a tile
+
+extern "C" int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv, int N,
+                                        int d, int vocab, float scale, int accumulate) {
+  const char* op = "embed_bwd_sorted";
+  if (dtype < 0 || dtype > 1) return refuse(op, "dtype is 0 or 1");
+  if (N < 0 || N > ROWS_MAX || d < 1 || vocab < 1) return refuse(op, "bad sizes");
+  if (!dV || (N && (!tok || !dh))) return refuse(op, "null pointer");
+  if ((N && lddh < d) || ldv < d) return refuse(op, "a leading dimension below d");
+  return rc_of(launch_embed_bwd_sorted((hipStream_t)stream, dtype, tok, dh, lddh, dV, ldv, N, d, vocab, scale, accumulate));
+}
+
+static_assert(RECURRENCE_STRIDE == OURO_RECURRENCE_STRIDE, "the boundary names the distance of the kept states");
+extern "C" size_t ouro_op_recurrence_scratch(int B, int T, int D) {
+  return B < 1 || T < 1 || T > ROWS_MAX || D < 1 ? 0 : recurrence_scratch_floats(B, T, D);
+}
+static const char* recurrence_refusal(int dtype, int B, int T, int D, int ldz, int ldx, int ldo, const float* scratch) {
+  if (dtype < 0 || dtype > 1) return "dtype is 0 or 1";
+  if (B < 1 || T < 1 || T > ROWS_MAX || D < 1) return "bad sizes";
+  if (ldz < D || ldx < D || ldo < D) return "a leading dimension below D";
+  if (!scratch && recurrence_scratch_floats(B, T, D)) return "these sizes need scratch";
+  return nullptr;
+}
+extern "C" int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
+                                      const float* h0, const int32_t* lens, void* h, int ldh, float* hT, float* states, float* scratch) {
+  const char* op = "recurrence_fwd";
+  if (const char* why = recurrence_refusal(dtype, B, T, D, ldz, ldx, ldh, scratch)) return refuse(op, why);
+  if (!z || !x || !h) return refuse(op, "null pointer");
+  RecurrenceDesc r;
+  memset(&r, 0, sizeof r);
+  r.B = B; r.T = T; r.D = D; r.z = z; r.ldz = ldz; r.x = x; r.ldx = ldx; r.lens = lens; r.states = states; r.scratch = scratch;
+  r.h0 = h0; r.h = h; r.ldh = ldh; r.hT = hT;
+  return rc_of(launch_recurrence((hipStream_t)stream, dtype, r));
+}
+extern "C" int ouro_op_recurrence_bwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
+                                      const float* states, const int32_t* lens, const void* dh, int lddh, const float* dhT, void* dz,
+                                      int lddz, void* dx, int lddx, float* dh0, float* scratch) {
+  const char* op = "recurrence_bwd";
+  if (const char* why = recurrence_refusal(dtype, B, T, D, ldz, ldx, lddh, scratch)) return refuse(op, why);
+  if (lddz < D || lddx < D) return refuse(op, "a leading dimension below D");
+  if (!z || !x || !states || !dh || !dz || !dx) return refuse(op, "null pointer");
+  RecurrenceDesc r;
+  memset(&r, 0, sizeof r);
+  r.B = B; r.T = T; r.D = D; r.z = z; r.ldz = ldz; r.x = x; r.ldx = ldx; r.lens = lens; r.states = const_cast<float*>(states);
+  r.scratch = scratch; r.dh = dh; r.lddh = lddh; r.dhT = dhT; r.dz = dz; r.lddz = lddz; r.dx = dx; r.lddx = lddx; r.dh0 = dh0;
+  return rc_of(launch_recurrence((hipStream_t)stream, dtype, r));
+}
+
 extern "C" int ouro_op_softmax_ce(void* stream, int dtype, const void* logits, int ld, const int32_t* tgt, void* G,
                                   int ldg, float* lse, float* rowloss, float* loss, int N, int vocab, int* flag) {
   if (!logits || !tgt || !G || !lse || !rowloss || !loss || !flag || N < 1 || ld < vocab || ldg < vocab) return OURO_E_ARG;

@@ -1,0 +1,49 @@
+"""What the entry points of the sorted embedding gradient, the recurrence and the orthogonalised update refuse before anything
+is enqueued (host only: no GPU is touched), with a message that names the operator."""
+import ctypes as C
+
+import pytest
+
+import paper_1909_06695_amd as P
+
+E_ARG = -2
+X = C.c_void_p(4096)                                             # an address that is never read
+
+
+def refused(rc, op):
+    assert rc == E_ARG
+    assert P.lib().ouro_last_error().startswith(op)
+
+
+EMBED = dict(dtype=0, tok=X, dh=X, lddh=8, dV=X, ldv=8, N=4, d=8, vocab=16, scale=1.0, accumulate=0)
+
+
+@pytest.mark.parametrize("change", [dict(dtype=2), dict(dtype=-1), dict(N=-1), dict(N=(1 << 30) + 1), dict(d=0), dict(vocab=0), dict(tok=None),
+                                    dict(dh=None), dict(dV=None), dict(lddh=7), dict(ldv=7)])
+def test_embed_bwd_sorted(change):
+    a = dict(EMBED, **change)
+    refused(P.lib().ouro_op_embed_bwd_sorted(None, *a.values()), b"embed_bwd_sorted")
+
+
+FWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, h0=None, lens=None, h=X, ldh=8, hT=None, states=None, scratch=None)
+BWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, states=X, lens=None, dh=X, lddh=8, dhT=None, dz=X, lddz=8, dx=X, lddx=8, dh0=None,
+           scratch=None)
+SIZES = [dict(dtype=2), dict(B=0), dict(T=0), dict(D=0), dict(T=(1 << 30) + 1), dict(z=None), dict(x=None), dict(ldz=7), dict(ldx=7), dict(T=100000)]
+
+
+@pytest.mark.parametrize("change", SIZES + [dict(h=None), dict(ldh=7)])
+def test_recurrence_fwd(change):
+    refused(P.lib().ouro_op_recurrence_fwd(None, *dict(FWD, **change).values()), b"recurrence_fwd")
+
+
+@pytest.mark.parametrize("change", SIZES + [dict(states=None), dict(dh=None), dict(dz=None), dict(dx=None), dict(lddh=7), dict(lddz=7), dict(lddx=7)])
+def test_recurrence_bwd(change):
+    refused(P.lib().ouro_op_recurrence_bwd(None, *dict(BWD, **change).values()), b"recurrence_bwd")
+
+
+def test_recurrence_scratch():
+    """No workspace for single tokens or where streams and channels fill the chip; sizes that are refused need none."""
+    size = P.lib().ouro_op_recurrence_scratch
+    assert size(64, 1, 1024) == 0 and size(64, 1000, 2048) == 0 and size(1, 64, 8) == 0
+    assert size(1, 65536, 512) > 0
+    assert size(0, 5, 5) == 0 and size(1, 0, 5) == 0 and size(1, 5, 0) == 0
