@@ -235,7 +235,7 @@ def _ptr(t):
 
 
 def _own(s):
-    import paper_1909_06695_amd as P
+    from paper_1909_06695_amd import binding as P
 
     L, c = P.lib(), s["case"]
     stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
