@@ -222,6 +222,19 @@ int ouro_op_update_groups(void* stream, int n, float* const* w, float* const* m,
                           const void* const* table, const int* entries, const int* tiles, int adam, float lr, float beta1, float beta2,
                           float eps, int64_t t);
 int ouro_op_update_tiles(int rows, int cols, int ld_out);
+/* Orthogonalised updates (the gradient side of an update of matrices; ouro_op_update with adam = 0 applies the result): for each of
+ * `batch` matrices U [rows, cols], o = scale * X after `steps` Newton-Schulz steps X <- a X + (b A + c A^2) X, A = X X^T (of the transpose
+ * where rows > cols), a, b, c = 3.4445, -4.7750, 2.0315, from X = U / (|U|_F + eps): five steps bring the singular values of U near 1.
+ * momentum NULL: U = g.  Else momentum (fp32, laid out as g) becomes mu momentum + g, and U is the new momentum, with nesterov != 0
+ * g + mu momentum.  g and o are of type T; matrix i begins sg (g, momentum) and so (o) elements behind matrix 0, rows ldg and ldo
+ * apart, any alignment of an element.  Matrices of o, and of momentum, must not overlap: they lie one after the other or side by side in
+ * wider rows (the parts of W_qkv).  o may be g.  A zero matrix stays zero (eps > 0); one with a NaN or infinity becomes NaN
+ * whole, the others of the batch are not affected.  The arithmetic is nearly that of fp32 (22-bit operands, fp32
+ * sums); entries of X below 2^-37 count as zero, which shows only where eps is many orders above |U|_F.  scratch: fp32, ouro_op_orthogonalize_scratch() floats, 16-byte aligned; 0 for sizes that are refused (padded to
+ * multiples of 64, rows * cols < 2^29). */
+int ouro_op_orthogonalize(void* stream, int dtype, int batch, int rows, int cols, const void* g, int ldg, long long sg, float* momentum, float mu,
+                          int nesterov, void* o, int ldo, long long so, float scale, float eps, int steps, float* scratch);
+size_t ouro_op_orthogonalize_scratch(int batch, int rows, int cols);
 /* dst (type T) = src (fp32), n elements; and back. */
 int ouro_op_from_f32(void* stream, int dtype, void* dst, const float* src, size_t n);
 int ouro_op_to_f32(void* stream, int dtype, float* dst, const void* src, size_t n);

@@ -128,6 +128,8 @@ def lib():
         "ouro_op_update_groups": (i32, [vp, i32, P(vp), P(vp), P(vp), P(vp), P(vp), P(vp), P(f32), P(vp), P(f32), P(sz), P(vp), P(i32), P(i32), i32,
                                         f32, f32, f32, f32, i64]),
         "ouro_op_update_tiles": (i32, [i32, i32, i32]),
+        "ouro_op_orthogonalize": (i32, [vp, i32, i32, i32, i32, vp, i32, C.c_longlong, vp, f32, i32, vp, i32, C.c_longlong, f32, f32, i32, vp]),
+        "ouro_op_orthogonalize_scratch": (sz, [i32, i32, i32]),
         "ouro_op_from_f32": (i32, [vp, i32, vp, vp, sz]),
         "ouro_op_to_f32": (i32, [vp, i32, vp, vp, sz]),
     }

@@ -319,4 +319,19 @@ struct UpdateTable { const TransposeEntry* dev; int entries, tiles; void* shadow
 int update_tiles(int rows, int cols, int ld_out);
 hipError_t launch_update_groups(hipStream_t s, const UpdateDesc* u, const UpdateTable* tab, int n);
 
+// Orthogonalised updates of `batch` matrices [rows, cols] of type T, sg elements (g and momentum, fp32) and so elements (o) apart:
+// momentum (null: none) = mu momentum + g, U = momentum (nesterov: g + mu momentum; without momentum g), o = scale NS(U / (|U| + eps))
+// with `steps` Newton-Schulz steps.  scratch: orthogonalize_scratch_floats(), 16-byte aligned.
+struct OrthogonalizeDesc {
+  int batch, rows, cols;
+  const void* g; int ldg; long long sg;
+  float* momentum; float mu; int nesterov;
+  void* o; int ldo; long long so;
+  float scale, eps;
+  int steps;
+  float* scratch;
+};
+size_t orthogonalize_scratch_floats(int batch, int rows, int cols);
+hipError_t launch_orthogonalize(hipStream_t s, int dtype, const OrthogonalizeDesc& d);
+
 }  // namespace ouro

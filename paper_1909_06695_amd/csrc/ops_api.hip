@@ -3,6 +3,7 @@
 #include "../../include/ouro.h"
 #include "../../include/ouro_ops.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -377,6 +378,38 @@ extern "C" int ouro_op_update_groups(void* stream, int n, float* const* w, float
     tab[i] = {(const TransposeEntry*)table[i], entries[i], tiles[i], shadowT[i]};
   }
   return rc_of(launch_update_groups((hipStream_t)stream, u, tab, n));
+}
+
+// Sizes that the kernels of the orthogonalisation take: a padded split matrix below 2 GiB, grids below 2^32 work items.
+static bool orthogonalize_sizes(int batch, int rows, int cols) {
+  if (batch < 1 || batch > 65535 || rows < 1 || cols < 1 || rows > ROWS_MAX || cols > ROWS_MAX) return false;
+  const long long mp = (std::min(rows, cols) + 63) / 64 * 64, np = (std::max(rows, cols) + 63) / 64 * 64;
+  return mp * np < 1ll << 29 && mp * np / 4096 * batch < 1ll << 24;
+}
+// Matrices `rows` long rows `ld` apart, `stride` elements apart: one after the other, or side by side in wider rows.
+static bool matrices_apart(int batch, int rows, int cols, int ld, long long stride) {
+  return batch == 1 || stride >= (long long)(rows - 1) * ld + cols || (stride >= cols && (batch - 1) * stride + cols <= ld);
+}
+extern "C" size_t ouro_op_orthogonalize_scratch(int batch, int rows, int cols) {
+  return orthogonalize_sizes(batch, rows, cols) ? orthogonalize_scratch_floats(batch, rows, cols) : 0;
+}
+extern "C" int ouro_op_orthogonalize(void* stream, int dtype, int batch, int rows, int cols, const void* g, int ldg, long long sg, float* momentum,
+                                     float mu, int nesterov, void* o, int ldo, long long so, float scale, float eps, int steps,
+                                     float* scratch) {
+  const char* op = "orthogonalize";
+  if (dtype < 0 || dtype > 1) return refuse(op, "dtype is 0 or 1");
+  if (!orthogonalize_sizes(batch, rows, cols)) return refuse(op, "bad sizes");
+  if (!g || !o || !scratch) return refuse(op, "null pointer");
+  if (ldg < cols || ldo < cols) return refuse(op, "a leading dimension below cols");
+  if (sg < 0 || !matrices_apart(batch, rows, cols, ldo, so) || (momentum && !matrices_apart(batch, rows, cols, ldg, sg)))
+    return refuse(op, "matrices that overlap");
+  if (!(eps >= 0.f) || steps < 1 || steps > 100) return refuse(op, "eps is not negative, steps 1 to 100");
+  if (reinterpret_cast<uintptr_t>(scratch) & 15) return refuse(op, "scratch is not 16-byte aligned");
+  OrthogonalizeDesc d;
+  memset(&d, 0, sizeof d);
+  d.batch = batch; d.rows = rows; d.cols = cols; d.g = g; d.ldg = ldg; d.sg = sg; d.momentum = momentum; d.mu = mu; d.nesterov = nesterov;
+  d.o = o; d.ldo = ldo; d.so = so; d.scale = scale; d.eps = eps; d.steps = steps; d.scratch = scratch;
+  return rc_of(launch_orthogonalize((hipStream_t)stream, dtype, d));
 }
 
 extern "C" int ouro_op_from_f32(void* stream, int dtype, void* dst, const float* src, size_t n) {

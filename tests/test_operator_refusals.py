@@ -47,3 +47,21 @@ def test_recurrence_scratch():
     assert size(64, 1, 1024) == 0 and size(64, 1000, 2048) == 0 and size(1, 64, 8) == 0
     assert size(1, 65536, 512) > 0
     assert size(0, 5, 5) == 0 and size(1, 0, 5) == 0 and size(1, 5, 0) == 0
+
+
+ORTHO = dict(dtype=0, batch=2, rows=16, cols=24, g=X, ldg=24, sg=384, momentum=None, mu=0.9, nesterov=0, o=X, ldo=24, so=384, scale=1.0, eps=1e-7,
+             steps=5, scratch=X)
+
+
+@pytest.mark.parametrize("change", [dict(dtype=2), dict(batch=0), dict(batch=65536), dict(rows=0), dict(cols=0), dict(g=None), dict(o=None),
+                                    dict(scratch=None), dict(scratch=C.c_void_p(4100)), dict(ldg=23), dict(ldo=23), dict(sg=-1), dict(so=383),
+                                    dict(so=0), dict(so=24), dict(so=24, ldo=47), dict(momentum=X, sg=0), dict(momentum=X, sg=100),
+                                    dict(eps=-1.0), dict(eps=float("nan")), dict(steps=0), dict(steps=101), dict(rows=32768, cols=32768, ldg=32768, ldo=32768)])
+def test_orthogonalize(change):
+    refused(P.lib().ouro_op_orthogonalize(None, *dict(ORTHO, **change).values()), b"orthogonalize")
+
+
+def test_orthogonalize_scratch():
+    size = P.lib().ouro_op_orthogonalize_scratch
+    assert size(1, 64, 256) > 0 and size(3, 100, 1) > 0 and size(2, 70, 500) == size(2, 500, 70)
+    assert size(0, 5, 5) == 0 and size(1, 0, 5) == 0 and size(1, 32768, 32768) == 0
