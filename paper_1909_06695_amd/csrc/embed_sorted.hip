@@ -11,25 +11,41 @@
 #include "common.h"
 #include "unaligned.h"
 
+#include <algorithm>
+
 namespace ouro {
 
 constexpr int ES_THREADS = 512, ES_WAVES = ES_THREADS / 64;
-constexpr int ES_LANES = 8;                                // lanes of a team: 128 bytes of a row of dh
-constexpr int ES_TEAMS = ES_THREADS / ES_LANES;
-constexpr int ES_CAP = 2048;                               // entries of the list; more ids than that go in parts
+constexpr int ES_TEAMS = ES_THREADS / STRIP_LANES;         // a team is the lanes of a strip: 128 bytes of a row of dh
+constexpr int ES_STEP = 256;                               // ids of a wave at a time, four neighbours a lane
+constexpr int ES_WAVE_CAP = 3 * ES_STEP, ES_CAP = ES_WAVES * ES_WAVE_CAP;     // entries of the list, of which each wave fills its part
 constexpr int ES_RANK = ES_THREADS;                        // longest list that is sorted by counting smaller entries
-constexpr int ES_BITS = 9, ES_BINS = 1 << ES_BITS;         // digit of the radix sort
-constexpr int ES_ROWS_MAX = 1 << 14;                       // matrix rows of a workgroup (one bit each, two digits)
-static_assert(ES_CAP % ES_THREADS == 0 && ES_BINS == ES_THREADS, "one bin a thread");
+constexpr int ES_BITS = 9, ES_BINS = 1 << ES_BITS;         // largest digit of the radix sort
+constexpr int ES_ROW_BITS = 14;                            // matrix rows of a workgroup: a bit each, two digits
+constexpr int ES_CLEARERS = 256;                           // workgroups that clear rows, one a CU
+static_assert(ES_BINS == ES_THREADS, "one bin a thread");
 
 struct EmbedSortedParams {
   const int32_t* tok; const void* dh; float* dV;
   size_t lddh, ldv;
   int N, d, vocab;
-  int log2R;
+  int slices, log2R;
+  int clearers, zero_rows;                                 // the first workgroups clear zero_rows rows each; 0: the sums are added
+  int n_bits, row_bits;                                    // an entry is (matrix row of the workgroup) << n_bits | position in ids
   float scale;
-  int accumulate;
 };
+
+// Four neighbouring ids, -1 behind the end.
+__device__ __forceinline__ int4 es_ids(const EmbedSortedParams& p, int at) {
+  int v[4] = {-1, -1, -1, -1};
+  if (at + 4 <= p.N) load_unaligned<int32_t, 4>(p.tok + at, v);
+  else if (at < p.N) {
+    v[0] = p.tok[at];
+    if (at + 1 < p.N) v[1] = p.tok[at + 1];
+    if (at + 2 < p.N) v[2] = p.tok[at + 2];
+  }
+  return make_int4(v[0], v[1], v[2], v[3]);
+}
 
 // Lanes of the wave whose `key` (bits wide) equals this lane's, among those of `in`.
 __device__ __forceinline__ uint64_t es_peers(uint32_t key, int bits, uint64_t in) {
@@ -40,200 +56,255 @@ __device__ __forceinline__ uint64_t es_peers(uint32_t key, int bits, uint64_t in
   return in;
 }
 
-// WHOLE: d is a whole number of 16-byte pieces of dh.
-template <typename T, bool WHOLE>
-__global__ __launch_bounds__(ES_THREADS) void embed_bwd_sorted_kernel(EmbedSortedParams p) {
-  constexpr int P = 16 / sizeof(T);                        // columns of a lane
-  constexpr int W = ES_LANES * P;                          // columns of the workgroup
-  __shared__ uint32_t row_a[ES_CAP], n_a[ES_CAP], row_b[ES_CAP], n_b[ES_CAP];
-  __shared__ uint32_t touched[ES_ROWS_MAX / 32];
-  __shared__ __align__(16) uint32_t hist_or_heads[ES_WAVES * ES_BINS];
-  __shared__ uint32_t wave_n[ES_WAVES];
-  static_assert(ES_TEAMS * W <= ES_WAVES * ES_BINS, "the heads fit the histogram's place");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t R = 1u << p.log2R, mine = blockIdx.x & (R - 1);
-  const int col = (blockIdx.x >> p.log2R) * W + (tid & (ES_LANES - 1)) * P;
-  const int ncol = max(0, min(P, p.d - col));
-  const int rows = (int)(((uint32_t)p.vocab - mine + R - 1) >> p.log2R);      // mine < vocab
-  const int team = tid / ES_LANES;
-  const uint64_t below = (1ull << lane) - 1;
-  const bool overwrite = !p.accumulate;
-  if (overwrite)
-    for (int i = tid; i < (rows + 31) / 32; i += ES_THREADS) touched[i] = 0;
-
-  // The ids [n0, n1) a wave looks at, 256 at a time: four neighbours a lane.
-  auto ids = [&](int n0, int n1, auto&& take) __attribute__((always_inline)) {
-    for (int n = n0; n < n1; n += 256) {
-      const int at = n + 4 * lane;
-      int v[4] = {-1, -1, -1, -1};
-      if (at + 4 <= n1) load_unaligned<int32_t, 4>(p.tok + at, v);
+// Clears the rows [z0, z1) without a token: neighbouring rows, whole, so that full cache lines are written.
+__device__ __forceinline__ void es_clear(const EmbedSortedParams& p, uint32_t z0, uint32_t z1, uint32_t* touched) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (uint32_t i = tid; i < (z1 - z0 + 31) / 32; i += ES_THREADS) touched[i] = 0;
+  __syncthreads();
+#pragma unroll 2
+  for (int n = 4 * tid; n < p.N; n += 4 * ES_THREADS) {
+    const int4 v = es_ids(p, n);
+    auto mark = [&](int id) __attribute__((always_inline)) {
+      const uint32_t r = (uint32_t)id - z0;
+      if (id >= 0 && r < z1 - z0) atomicOr(&touched[r >> 5], 1u << (r & 31));
+    };
+    mark(v.x); mark(v.y); mark(v.z); mark(v.w);
+  }
+  __syncthreads();
+  int lanes = 1;                                           // of a row, 16 bytes each
+  while (lanes < 64 && lanes * 4 < p.d) lanes *= 2;
+  const int rows = 64 / lanes, c0 = lane % lanes * 4;
+  const float zero[4] = {};
+  for (uint32_t i = wave * rows + lane / lanes; i < z1 - z0; i += ES_WAVES * rows) {
+    if (touched[i >> 5] >> (i & 31) & 1) continue;
+    float* out = p.dV + (z0 + i) * p.ldv;
+    for (int c = c0; c < p.d; c += lanes * 4) {
+      if (c + 4 <= p.d) store_unaligned<float, 4>(out + c, zero);
       else
-        for (int j = 0; j < 4; ++j)
-          if (at + j < n1) v[j] = p.tok[at + j];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) take(at + j, (uint32_t)v[j], (uint32_t)v[j] < (uint32_t)p.vocab && ((uint32_t)v[j] & (R - 1)) == mine);
+        for (int e = c; e < p.d; ++e) out[e] = 0.f;
     }
-  };
-  // Puts the entries among the ids [c0, c1) into row_a, n_a and returns their number (in every thread); with count_only only counts.
-  auto collect = [&](int c0, int c1, bool count_only) __attribute__((always_inline)) {
-    const int per = ((c1 - c0 + ES_WAVES - 1) / ES_WAVES + 3) & ~3;
-    const int n0 = min(c1, c0 + wave * per), n1 = min(c1, n0 + per);
-    uint32_t k = 0;
-    ids(n0, n1, [&](int, uint32_t, bool on) { k += (uint32_t)__popcll(__ballot(on)); });
-    if (lane == 0) wave_n[wave] = k;
-    __syncthreads();
-    uint32_t at = 0, total = 0;
-    for (int w = 0; w < ES_WAVES; ++w) {
-      if (w == wave) at = total;
-      total += wave_n[w];
-    }
-    if (!count_only && total <= ES_CAP)
-      ids(n0, n1, [&](int n, uint32_t v, bool on) {
-        const uint64_t m = __ballot(on);
-        if (on) {
-          const uint32_t slot = at + (uint32_t)__popcll(m & below);
-          row_a[slot] = v >> p.log2R;
-          n_a[slot] = (uint32_t)n;
-        }
-        at += (uint32_t)__popcll(m);
-      });
-    __syncthreads();
-    return (int)total;
-  };
+  }
+}
 
-  bool first = true;
-  int chunk = p.N;
-  for (int c0 = 0; c0 < p.N || first; c0 += chunk) {
-    int m = collect(c0, min(p.N, c0 + chunk), false);
-    if (m > ES_CAP) {                                      // more than the list holds: in parts that cannot be
-      chunk = ES_CAP;
-      m = collect(c0, min(p.N, c0 + chunk), false);
+// WHOLE: see lane_columns.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSortedParams p) {
+  constexpr int P = 16 / sizeof(T);                        // columns of a lane
+  constexpr int W = STRIP_LANES * P;                       // columns of the workgroup
+  __shared__ __align__(16) uint32_t list_a[ES_CAP], list_b[ES_CAP];
+  __shared__ __align__(16) uint32_t hist_or_heads[ES_WAVES * ES_BINS];
+  __shared__ uint32_t seen[1 << (ES_ROW_BITS - 5)];
+  __shared__ uint32_t count[ES_WAVES], bins[ES_WAVES];
+  __shared__ uint8_t through[ES_WAVES];
+  static_assert(ES_TEAMS * W <= ES_WAVES * ES_BINS, "the heads fit the histogram's place");
+  if ((int)blockIdx.x < p.clearers) {
+    const uint32_t z0 = (uint32_t)min((uint64_t)blockIdx.x * p.zero_rows, (uint64_t)p.vocab), z1 = (uint32_t)min((uint64_t)z0 + p.zero_rows, (uint64_t)p.vocab);
+    es_clear(p, z0, z1, list_a);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int4 next = es_ids(p, wave * ES_STEP + 4 * lane);
+  const uint32_t block = blockIdx.x - p.clearers, R = 1u << p.log2R, mine = block / p.slices;
+  const LaneColumns own = lane_columns<P, WHOLE>(block % p.slices, lane % STRIP_LANES, p.d);
+  const int team = tid / STRIP_LANES;
+  const uint64_t below = (1ull << lane) - 1;
+  const bool overwrite = p.clearers > 0;
+  for (int i = tid; i < 1 << max(0, p.row_bits - 5); i += ES_THREADS) seen[i] = 0;
+
+  bool first = true, end = false;
+  int n0 = 0;                                              // ids before n0 have been looked at
+  while (!end) {
+    // ---- the entries among the ids, in order for each wave
+    const int n_base = n0;
+    int k = 0;
+    for (int steps = 0;; ++steps) {
+      end = n0 >= p.N;
+      if (end || n0 - n_base > (1 << p.n_bits) - ES_WAVES * ES_STEP) break;
+      if (steps >= ES_WAVE_CAP / ES_STEP && __syncthreads_or(k > ES_WAVE_CAP - ES_STEP)) break;
+      const int4 v = next;
+      const int at = n0 + wave * ES_STEP + 4 * lane;
+      next = es_ids(p, at + ES_WAVES * ES_STEP);
+      auto take = [&](uint32_t id, int n) __attribute__((always_inline)) {
+        const bool on = id < (uint32_t)p.vocab && (id & (R - 1)) == mine;
+        const uint64_t all = __ballot(on);
+        if (on) list_a[wave * ES_WAVE_CAP + k + (int)__popcll(all & below)] = id >> p.log2R << p.n_bits | (uint32_t)n;
+        k += (int)__popcll(all);
+      };
+      take(v.x, at - n_base); take(v.y, at + 1 - n_base); take(v.z, at + 2 - n_base); take(v.w, at + 3 - n_base);
+      n0 += ES_WAVES * ES_STEP;
     }
-    // ---- stable sort by row
-    const uint32_t *row = row_a, *ns = n_a;
+    if (lane == 0) count[wave] = (uint32_t)k;
+    __syncthreads();
+    int m = 0, at = 0;
+#pragma unroll
+    for (int w = 0; w < ES_WAVES; ++w) {
+      at += w < wave ? (int)count[w] : 0;
+      m += (int)count[w];
+    }
+    for (int i = lane; i < k; i += 64) list_b[at + i] = list_a[wave * ES_WAVE_CAP + i];
+    __syncthreads();
+    // ---- a stable sort by row
+    const uint32_t* key = list_b;
     if (m > 1 && m <= ES_RANK) {
-      if (tid < m) {
-        const uint32_t r = row_a[tid];
+      if (tid < m) {                                       // entries differ: the place of one is the number of smaller ones
+        const uint32_t e = list_b[tid];
         uint32_t rank = 0;
-        for (int j = 0; j < m; ++j) rank += (uint32_t)(row_a[j] < r || (row_a[j] == r && j < tid));
-        row_b[rank] = r;
-        n_b[rank] = n_a[tid];
+        int j = 0;
+#pragma unroll 4
+        for (; j + 4 <= m; j += 4) {
+          const uint4 o = *reinterpret_cast<const uint4*>(list_b + j);
+          rank += (uint32_t)(o.x < e) + (uint32_t)(o.y < e) + (uint32_t)(o.z < e) + (uint32_t)(o.w < e);
+        }
+        for (; j < m; ++j) rank += (uint32_t)(list_b[j] < e);
+        list_a[rank] = e;
       }
-      row = row_b; ns = n_b;
+      key = list_a;
       __syncthreads();
     } else if (m > ES_RANK) {
-      uint32_t* hist = hist_or_heads;                      // [wave][bin]
+      uint32_t* hist = hist_or_heads + wave * ES_BINS;     // [wave][bin]
       const int per = (m + ES_THREADS - 1) / ES_THREADS * 64, e0 = min(m, wave * per), e1 = min(m, e0 + per);
-      uint32_t *ra = row_a, *na = n_a, *rb = row_b, *nb = n_b;
-      for (int shift = 0; shift == 0 || ((rows - 1) >> shift) > 0; shift += ES_BITS) {
-        for (int i = tid; i < ES_WAVES * ES_BINS; i += ES_THREADS) hist[i] = 0;
-        __syncthreads();
-        for (int i = e0 + lane; i < e1; i += 64) atomicAdd(&hist[wave * ES_BINS + ((ra[i] >> shift) & (ES_BINS - 1))], 1u);
+      uint32_t *from = list_b, *to = list_a;
+      const int passes = (max(1, p.row_bits) + ES_BITS - 1) / ES_BITS, digit = (max(1, p.row_bits) + passes - 1) / passes;
+      for (int shift = p.n_bits; shift < p.n_bits + max(1, p.row_bits); shift += digit) {
+        const uint32_t mask = (1u << digit) - 1;
+        for (int i = lane; i < ES_BINS / 4; i += 64) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = e0; i < e1; i += 64) {                // how many a bin
+          const bool on = i + lane < e1;
+          const uint32_t bin = on ? (from[i + lane] >> shift) & mask : 0;
+          const uint64_t peers = es_peers(bin, digit, __ballot(on));
+          if (on && !(peers & below)) hist[bin] += (uint32_t)__popcll(peers);
+          __builtin_amdgcn_wave_barrier();
+        }
         __syncthreads();
         uint32_t sum = 0;                                  // this thread's bin over the waves, then over the bins before
-        for (int w = 0; w < ES_WAVES; ++w) sum += hist[w * ES_BINS + tid];
+#pragma unroll
+        for (int w = 0; w < ES_WAVES; ++w) sum += hist_or_heads[w * ES_BINS + tid];
         uint32_t incl = sum;
+#pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
           const uint32_t y = __shfl_up(incl, o, 64);
           if (lane >= o) incl += y;
         }
-        if (lane == 63) wave_n[wave] = incl;
+        if (lane == 63) bins[wave] = incl;
         __syncthreads();
         uint32_t base = incl - sum;
-        for (int w = 0; w < wave; ++w) base += wave_n[w];
+#pragma unroll
+        for (int w = 0; w < ES_WAVES; ++w) base += w < wave ? bins[w] : 0;
+#pragma unroll
         for (int w = 0; w < ES_WAVES; ++w) {
-          const uint32_t k = hist[w * ES_BINS + tid];
-          hist[w * ES_BINS + tid] = base;
-          base += k;
+          const uint32_t had = hist_or_heads[w * ES_BINS + tid];
+          hist_or_heads[w * ES_BINS + tid] = base;
+          base += had;
         }
         __syncthreads();
-        for (int i0 = e0; i0 < e1; i0 += 64) {
-          const bool on = i0 + lane < e1;
-          const uint32_t r = on ? ra[i0 + lane] : 0, n = on ? na[i0 + lane] : 0, bin = (r >> shift) & (ES_BINS - 1);
-          const uint64_t peers = es_peers(bin, ES_BITS, __ballot(on));
+        for (int i = e0; i < e1; i += 64) {                // where each goes
+          const bool on = i + lane < e1;
+          const uint32_t e = on ? from[i + lane] : 0, bin = (e >> shift) & mask;
+          const uint64_t peers = es_peers(bin, digit, __ballot(on));
+          uint32_t place = 0;
           if (on) {
-            const uint32_t at = hist[wave * ES_BINS + bin] + (uint32_t)__popcll(peers & below);
-            rb[at] = r;
-            nb[at] = n;
+            place = hist[bin];
+            to[place + (uint32_t)__popcll(peers & below)] = e;
           }
           __builtin_amdgcn_wave_barrier();
-          if (on && !(peers & below)) hist[wave * ES_BINS + bin] += (uint32_t)__popcll(peers);
+          if (on && !(peers & below)) hist[bin] = place + (uint32_t)__popcll(peers);
           __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
-        uint32_t* t = ra; ra = rb; rb = t;
-        t = na; na = nb; nb = t;
+        uint32_t* t = from; from = to; to = t;
       }
-      row = ra; ns = na;
+      key = from;
     }
-    // ---- rows without a token
-    if (first && overwrite) {
-      for (int i = tid; i < m; i += ES_THREADS) atomicOr(&touched[row[i] >> 5], 1u << (row[i] & 31));
-      __syncthreads();
-      const float zero[P] = {};
-      for (int i = team; i < rows; i += ES_TEAMS)
-        if (!(touched[i >> 5] >> (i & 31) & 1)) store_columns<float, P, WHOLE>(p.dV + ((size_t)i << p.log2R | mine) * p.ldv + col, zero, ncol);
-    }
-    // ---- sums
+    // ---- sums: a team takes an equal piece of the sorted list
     float* heads = reinterpret_cast<float*>(hist_or_heads);    // [team][W]: a team's part of a sum that an earlier team owns
     const int per = (m + ES_TEAMS - 1) / ES_TEAMS, s = min(m, team * per), e = min(m, s + per);
-    float acc[P] = {};
+    const uint32_t mask_n = (1u << p.n_bits) - 1;
+    float acc[P] = {}, old[P] = {};                        // of the sum under way; what the matrix holds
+    auto place = [&](uint32_t r) __attribute__((always_inline)) { return p.dV + ((size_t)r << p.log2R | mine) * p.ldv + own.col; };
     auto write = [&](uint32_t r) __attribute__((always_inline)) {
-      float* out = p.dV + ((size_t)r << p.log2R | mine) * p.ldv + col;
-      float v[P] = {};
-      if (!overwrite || !first) load_columns<float, P, WHOLE>(out, v, ncol);
 #pragma unroll
-      for (int j = 0; j < P; ++j) v[j] = fmaf(p.scale, acc[j], v[j]);
-      store_columns<float, P, WHOLE>(out, v, ncol);
+      for (int j = 0; j < P; ++j) old[j] = fmaf(p.scale, acc[j], old[j]);
+      store_columns<float, P, WHOLE>(place(r), old, own.n);
     };
-    bool pending = false;                                  // the last sum goes on in the next team's piece
+    bool pending = false, middle = false;                  // the last sum goes on in the next team's piece, and began here or before
+    uint32_t cur = 0;
     if (s < e) {
-      const T* dh = reinterpret_cast<const T*>(p.dh) + col;
-      uint32_t cur = row[s];
-      bool head = s > 0 && row[s - 1] == cur;
-      auto flush = [&]() __attribute__((always_inline)) {
-        if (head) {
-#pragma unroll
-          for (int j = 0; j < P; ++j) heads[team * W + (tid & (ES_LANES - 1)) * P + j] = acc[j];
-        } else {
-          write(cur);
-        }
-        head = false;
-#pragma unroll
-        for (int j = 0; j < P; ++j) acc[j] = 0.f;
-      };
-      constexpr int U = 8;                                 // rows requested together
+      const T* dh = reinterpret_cast<const T*>(p.dh) + n_base * p.lddh + own.col;
+      cur = key[s] >> p.n_bits;
+      bool head = s > 0 && key[s - 1] >> p.n_bits == cur;
+      uint32_t before = head ? cur : ~0u;                  // row of the entry before the ones requested
+      constexpr int U = 4;                                 // rows requested together, with the matrix rows of sums that begin
       for (int i = s; i < e; i += U) {
-        float x[U][P] = {};
+        UnalignedPack<T, P> x[U] = {};
+        UnalignedPack<float, P> had[U] = {};
+        uint32_t r[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (i + u < e) load_columns<T, P, WHOLE>(dh + ns[i + u] * p.lddh, x[u], ncol);
+        for (int u = 0; u < U; ++u) {
+          const uint32_t entry = key[min(i + u, e - 1)];
+          r[u] = entry >> p.n_bits;
+          if (i + u < e) {
+            load_raw_columns<T, P, WHOLE>(dh + (size_t)(entry & mask_n) * p.lddh, x[u], own.n);
+            if (r[u] != before && (!overwrite || (!first && (seen[r[u] >> 5] >> (r[u] & 31) & 1)))) load_raw_columns<float, P, WHOLE>(place(r[u]), had[u], own.n);
+          }
+          before = r[u];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (i + u < e) {
-            const uint32_t r = row[i + u];
-            if (r != cur) { flush(); cur = r; }
+            const bool change = r[u] != cur;
+            if (change) {
+              if (head) {
 #pragma unroll
-            for (int j = 0; j < P; ++j) acc[j] += x[u][j];
+                for (int j = 0; j < P; ++j) heads[team * W + (lane % STRIP_LANES) * P + j] = acc[j];
+              } else {
+                write(cur);
+              }
+              head = false;
+              cur = r[u];
+            }
+            if (change || (i + u == s && !head)) {
+#pragma unroll
+              for (int j = 0; j < P; ++j) { acc[j] = 0.f; old[j] = had[u].v[j]; }
+            }
+#pragma unroll
+            for (int j = 0; j < P; ++j) acc[j] += to_f32(x[u].v[j]);
           }
       }
-      pending = e < m && row[e] == cur && !head;
-      if (!pending) flush();
+      const bool goes_on = e < m && key[e] >> p.n_bits == cur;
+      pending = goes_on && !head;
+      middle = goes_on && head;
+      if (head) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) heads[team * W + (lane % STRIP_LANES) * P + j] = acc[j];
+      } else if (!pending) {
+        write(cur);
+      }
+    }
+    const uint64_t middles = __ballot(middle);             // one bit a team
+    if (lane == 0) {
+      uint32_t bits = 0;
+      for (int t = 0; t < 64 / STRIP_LANES; ++t) bits |= (uint32_t)(middles >> (t * STRIP_LANES) & 1) << t;
+      through[wave] = (uint8_t)bits;
     }
     __syncthreads();
     if (pending) {
-      const uint32_t cur = row[e];
-      for (int t = team + 1;; ++t) {
+      uint64_t mask = 0;
 #pragma unroll
-        for (int j = 0; j < P; ++j) acc[j] += heads[t * W + (tid & (ES_LANES - 1)) * P + j];
-        const int end = (t + 1) * per;
-        if (end >= m || row[end] != cur) break;
-      }
+      for (int w = 0; w < ES_WAVES; ++w) mask |= (uint64_t)through[w] << (w * 8);
+      const int more = (int)__ffsll((unsigned long long)~(mask >> team >> 1));    // teams that hold the rest
+      const float* h = heads + (team + 1) * W + (lane % STRIP_LANES) * P;
+#pragma unroll 4
+      for (int t = 0; t < more; ++t)
+#pragma unroll
+        for (int j = 0; j < P; ++j) acc[j] += h[t * W + j];
       write(cur);
     }
+    if (!end) {
+      __syncthreads();
+      for (int i = tid; i < m; i += ES_THREADS) atomicOr(&seen[key[i] >> p.n_bits >> 5], 1u << (key[i] >> p.n_bits & 31));
+      __syncthreads();
+    }
     first = false;
-    __syncthreads();
-    if (chunk >= p.N) break;
   }
 }
 
@@ -241,19 +312,24 @@ hipError_t launch_embed_bwd_sorted(hipStream_t s, int dtype, const int32_t* tok,
                                    int vocab, float scale, int accumulate) {
   EmbedSortedParams p;
   memset(&p, 0, sizeof p);
-  p.tok = tok; p.dh = dh; p.dV = dV; p.lddh = lddh; p.ldv = ldv; p.N = N; p.d = d; p.vocab = vocab; p.scale = scale; p.accumulate = accumulate;
-  const int W = ES_LANES * 16 / (dtype == 1 ? 2 : 4), slices = (d + W - 1) / W;
-  // About 1024 workgroups, four matrix rows each at least; as many as keep a workgroup's rows within its bit map.
-  while (((long long)slices << p.log2R) < 1024 && (4ll << p.log2R) < vocab) ++p.log2R;
-  while (((long long)ES_ROWS_MAX << p.log2R) < vocab) ++p.log2R;
-  const long long blocks = (long long)slices << p.log2R;
+  p.tok = tok; p.dh = dh; p.dV = dV; p.lddh = lddh; p.ldv = ldv; p.N = N; p.d = d; p.vocab = vocab; p.scale = scale;
+  p.slices = dtype == 1 ? strip_count<8>(d) : strip_count<4>(d);
+  // As many workgroups as the chip holds at once, two a CU, of which half clear rows where the matrix is overwritten; four
+  // matrix rows each at least, and as many workgroups as keep the bit maps within their sizes.
+  p.clearers = accumulate ? 0 : std::min((vocab + 3) / 4, std::max(ES_CLEARERS, (int)((vocab + 32ll * ES_CAP - 1) / (32ll * ES_CAP))));
+  p.zero_rows = accumulate ? 0 : (vocab + p.clearers - 1) / p.clearers;
+  while (((long long)p.slices << (p.log2R + 1)) <= (accumulate ? 512 : 256) && (4ll << p.log2R) < vocab) ++p.log2R;
+  while ((1ll << ES_ROW_BITS << p.log2R) < vocab) ++p.log2R;
+  while ((1ll << p.row_bits << p.log2R) < vocab) ++p.row_bits;
+  p.n_bits = std::min(30, 32 - p.row_bits);
+  const long long blocks = ((long long)p.slices << p.log2R) + p.clearers;
   if (blocks * ES_THREADS >> 32) return hipErrorInvalidValue;
   dim3 grid((unsigned)blocks), block(ES_THREADS);
   if (dtype == 1) {
-    if (d % 8 == 0) hipLaunchKernelGGL((embed_bwd_sorted_kernel<bf16_t, true>), grid, block, 0, s, p);
+    if (d >= 8) hipLaunchKernelGGL((embed_bwd_sorted_kernel<bf16_t, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((embed_bwd_sorted_kernel<bf16_t, false>), grid, block, 0, s, p);
   } else {
-    if (d % 4 == 0) hipLaunchKernelGGL((embed_bwd_sorted_kernel<float, true>), grid, block, 0, s, p);
+    if (d >= 4) hipLaunchKernelGGL((embed_bwd_sorted_kernel<float, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((embed_bwd_sorted_kernel<float, false>), grid, block, 0, s, p);
   }
   return hipGetLastError();

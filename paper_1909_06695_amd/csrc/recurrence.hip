@@ -18,7 +18,7 @@
 
 namespace ouro {
 
-constexpr int RC_LANES = 8, RC_ROWS = 64 / RC_LANES;       // of a wave: 8 rows of 8 lanes, 16 bytes a lane
+constexpr int RC_LANES = STRIP_LANES, RC_ROWS = 64 / RC_LANES;       // of a wave: 8 rows of 8 lanes, 16 bytes a lane
 constexpr int RC_WAVES = 8;                                // most waves of a workgroup
 template <typename T> struct RcShape {
   static constexpr int P = 16 / sizeof(T);                 // channels of a lane
@@ -53,7 +53,7 @@ struct RcPlace {
   int b, seg, col, ncol, wave, row, lane8, waves, t0, t1, len;     // t0, t1: the segment's steps
   size_t base;                                             // row of step 0
 };
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ RcPlace rc_place(const RecurrenceParams& p) {
   RcPlace a;
   const int strip = blockIdx.x % p.strips, rest = blockIdx.x / p.strips;
@@ -63,8 +63,9 @@ __device__ __forceinline__ RcPlace rc_place(const RecurrenceParams& p) {
   a.row = (threadIdx.x & 63) / RC_LANES;
   a.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   a.waves = blockDim.x >> 6;
-  a.col = strip * RcShape<T>::W + a.lane8 * RcShape<T>::P;
-  a.ncol = max(0, min(RcShape<T>::P, p.D - a.col));
+  const LaneColumns own = lane_columns<RcShape<T>::P, WHOLE>(strip, a.lane8, p.D);
+  a.col = own.col;
+  a.ncol = own.n;
   a.t0 = a.seg * p.seg_steps;
   a.t1 = min(p.T, a.t0 + p.seg_steps);
   a.len = p.lens ? max(0, min(p.T, p.lens[a.b])) : p.T;
@@ -138,12 +139,12 @@ __device__ __forceinline__ void rc_leave_map(const RecurrenceParams& p, const Rc
   store_columns<float, P, WHOLE>(rc_map(p, a, a.seg) + p.D, state, a.ncol);
 }
 
-// MAPS: only the map of the segment.  WHOLE: D is a whole number of 16-byte pieces.
+// MAPS: only the map of the segment.  WHOLE: see lane_columns.
 template <typename T, bool WHOLE, bool MAPS>
 __global__ __launch_bounds__(64 * RC_WAVES) void recurrence_fwd_kernel(RecurrenceParams p) {
   constexpr int P = RcShape<T>::P, L = RcShape<T>::L, W = RcShape<T>::W, STEPS = RcShape<T>::STEPS;
   __shared__ float sA[2][RC_WAVES][W], sH[2][RC_WAVES][W];
-  const RcPlace a = rc_place<T>(p);
+  const RcPlace a = rc_place<T, WHOLE>(p);
   if (MAPS && a.seg == p.segs - 1) return;                 // nothing starts behind the last segment
   const T* z = reinterpret_cast<const T*>(p.z) + a.col;
   const T* x = reinterpret_cast<const T*>(p.x) + a.col;
@@ -220,7 +221,7 @@ template <typename T, bool WHOLE, bool MAPS>
 __global__ __launch_bounds__(64 * RC_WAVES) void recurrence_bwd_kernel(RecurrenceParams p) {
   constexpr int P = RcShape<T>::P, L = RcShape<T>::L, W = RcShape<T>::W, STEPS = RcShape<T>::STEPS;
   __shared__ float sA[2][RC_WAVES][W], sH[2][RC_WAVES][W], sQ[2][RC_WAVES][W];
-  const RcPlace a = rc_place<T>(p);
+  const RcPlace a = rc_place<T, WHOLE>(p);
   if (MAPS && a.seg == 0) return;                          // nothing starts before the first segment
   const T* z = reinterpret_cast<const T*>(p.z) + a.col;
   const T* x = reinterpret_cast<const T*>(p.x) + a.col;
@@ -324,8 +325,8 @@ __global__ __launch_bounds__(64 * RC_WAVES) void recurrence_bwd_kernel(Recurrenc
 struct RcPlan { int strips, waves, segs, seg_steps; };
 static RcPlan rc_plan(int dtype, int B, int T, int D) {
   RcPlan r;
-  const int W = dtype == 1 ? RcShape<bf16_t>::W : RcShape<float>::W, steps = dtype == 1 ? RcShape<bf16_t>::STEPS : RcShape<float>::STEPS;
-  r.strips = (D + W - 1) / W;
+  const int steps = dtype == 1 ? RcShape<bf16_t>::STEPS : RcShape<float>::STEPS;
+  r.strips = dtype == 1 ? strip_count<8>(D) : strip_count<4>(D);
   r.waves = 1;
   while (r.waves < RC_WAVES && (long long)r.waves * steps < T) r.waves *= 2;
   const int tile = r.waves * steps, tiles = (int)(((long long)T + tile - 1) / tile);
@@ -372,8 +373,8 @@ hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r) 
   p.h = r.h; p.dz = r.dz; p.dx = r.dx; p.ldh = r.ldh; p.lddz = r.lddz; p.lddx = r.lddx;
   p.hT = r.hT; p.dh0 = r.dh0; p.states = r.states; p.maps = r.scratch;
   const bool backward = r.dz != nullptr;
-  if (dtype == 1) return r.D % 8 == 0 ? rc_launch<bf16_t, true>(s, (unsigned)blocks, plan.waves, p, backward) : rc_launch<bf16_t, false>(s, (unsigned)blocks, plan.waves, p, backward);
-  return r.D % 4 == 0 ? rc_launch<float, true>(s, (unsigned)blocks, plan.waves, p, backward) : rc_launch<float, false>(s, (unsigned)blocks, plan.waves, p, backward);
+  if (dtype == 1) return r.D >= 8 ? rc_launch<bf16_t, true>(s, (unsigned)blocks, plan.waves, p, backward) : rc_launch<bf16_t, false>(s, (unsigned)blocks, plan.waves, p, backward);
+  return r.D >= 4 ? rc_launch<float, true>(s, (unsigned)blocks, plan.waves, p, backward) : rc_launch<float, false>(s, (unsigned)blocks, plan.waves, p, backward);
 }
 
 }  // namespace ouro
