@@ -19,9 +19,12 @@ constexpr int ES_THREADS = 512, ES_WAVES = ES_THREADS / 64;
 constexpr int ES_TEAMS = ES_THREADS / STRIP_LANES;         // a team is the lanes of a strip: 128 bytes of a row of dh
 constexpr int ES_STEP = 256;                               // ids of a wave at a time, four neighbours a lane
 constexpr int ES_WAVE_CAP = 3 * ES_STEP, ES_CAP = ES_WAVES * ES_WAVE_CAP;     // entries of the list, of which each wave fills its part
-constexpr int ES_RANK = ES_THREADS;                        // longest list that is sorted by counting smaller entries
+constexpr int ES_RANK = ES_THREADS;                        // longest list that is sorted from runs of 64
+constexpr int ES_COUNT = 128;                              // longest list that is sorted by counting alone (its cost grows with the square: 128 entries 1.5 us, 400 5.5
+                                                           // against 3.5 from runs)
 constexpr int ES_BITS = 9, ES_BINS = 1 << ES_BITS;         // largest digit of the radix sort
 constexpr int ES_ROW_BITS = 14;                            // matrix rows of a workgroup: a bit each, two digits
+constexpr int ES_COLD_COST = 3;                            // rows summed in the time of one that is a sum by itself
 constexpr int ES_CLEARERS = 256;                           // workgroups that clear rows, one a CU
 static_assert(ES_BINS == ES_THREADS, "one bin a thread");
 
@@ -47,6 +50,10 @@ __device__ __forceinline__ int4 es_ids(const EmbedSortedParams& p, int at) {
   return make_int4(v[0], v[1], v[2], v[3]);
 }
 
+// How many lanes below this one are in the set.
+__device__ __forceinline__ int es_below(uint64_t set) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0));
+}
 // Lanes of the wave whose `key` (bits wide) equals this lane's, among those of `in`.
 __device__ __forceinline__ uint64_t es_peers(uint32_t key, int bits, uint64_t in) {
   for (int b = 0; b < bits; ++b) {
@@ -86,8 +93,8 @@ __device__ __forceinline__ void es_clear(const EmbedSortedParams& p, uint32_t z0
   }
 }
 
-// WHOLE: see lane_columns.
-template <typename T, bool WHOLE>
+// WHOLE: see lane_columns.  ADD: onto what the matrix holds.
+template <typename T, bool WHOLE, bool ADD>
 __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSortedParams p) {
   constexpr int P = 16 / sizeof(T);                        // columns of a lane
   constexpr int W = STRIP_LANES * P;                       // columns of the workgroup
@@ -103,12 +110,9 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int4 next = es_ids(p, wave * ES_STEP + 4 * lane);
   const uint32_t block = blockIdx.x - p.clearers, R = 1u << p.log2R, mine = block / p.slices;
   const LaneColumns own = lane_columns<P, WHOLE>(block % p.slices, lane % STRIP_LANES, p.d);
   const int team = tid / STRIP_LANES;
-  const uint64_t below = (1ull << lane) - 1;
-  const bool overwrite = p.clearers > 0;
   for (int i = tid; i < 1 << max(0, p.row_bits - 5); i += ES_THREADS) seen[i] = 0;
 
   bool first = true, end = false;
@@ -117,21 +121,28 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
     // ---- the entries among the ids, in order for each wave
     const int n_base = n0;
     int k = 0;
-    for (int steps = 0;; ++steps) {
-      end = n0 >= p.N;
-      if (end || n0 - n_base > (1 << p.n_bits) - ES_WAVES * ES_STEP) break;
-      if (steps >= ES_WAVE_CAP / ES_STEP && __syncthreads_or(k > ES_WAVE_CAP - ES_STEP)) break;
-      const int4 v = next;
-      const int at = n0 + wave * ES_STEP + 4 * lane;
-      next = es_ids(p, at + ES_WAVES * ES_STEP);
-      auto take = [&](uint32_t id, int n) __attribute__((always_inline)) {
-        const bool on = id < (uint32_t)p.vocab && (id & (R - 1)) == mine;
-        const uint64_t all = __ballot(on);
-        if (on) list_a[wave * ES_WAVE_CAP + k + (int)__popcll(all & below)] = id >> p.log2R << p.n_bits | (uint32_t)n;
-        k += (int)__popcll(all);
-      };
-      take(v.x, at - n_base); take(v.y, at + 1 - n_base); take(v.z, at + 2 - n_base); take(v.w, at + 3 - n_base);
-      n0 += ES_WAVES * ES_STEP;
+    for (bool full = false; !full;) {
+      constexpr int AHEAD = 4;                             // steps requested together
+      int4 v[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) v[u] = es_ids(p, n0 + (u * ES_WAVES + wave) * ES_STEP + 4 * lane);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        end = n0 >= p.N;
+        const int gone = n0 - n_base;
+        full = full || end || gone > (1 << p.n_bits) - ES_WAVES * ES_STEP;
+        if (!full && gone >= ES_WAVES * ES_WAVE_CAP) full = __syncthreads_or(k > ES_WAVE_CAP - ES_STEP);
+        if (full) continue;
+        const int at = gone + wave * ES_STEP + 4 * lane;
+        auto take = [&](uint32_t id, int n) __attribute__((always_inline)) {
+          const bool on = id < (uint32_t)p.vocab && (id & (R - 1)) == mine;
+          const uint64_t all = __ballot(on);
+          if (on) list_a[wave * ES_WAVE_CAP + k + es_below(all)] = id >> p.log2R << p.n_bits | (uint32_t)n;
+          k += (int)__popcll(all);
+        };
+        take(v[u].x, at); take(v[u].y, at + 1); take(v[u].z, at + 2); take(v[u].w, at + 3);
+        n0 += ES_WAVES * ES_STEP;
+      }
     }
     if (lane == 0) count[wave] = (uint32_t)k;
     __syncthreads();
@@ -143,27 +154,87 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
     }
     for (int i = lane; i < k; i += 64) list_b[at + i] = list_a[wave * ES_WAVE_CAP + i];
     __syncthreads();
-    // ---- a stable sort by row
-    const uint32_t* key = list_b;
-    if (m > 1 && m <= ES_RANK) {
-      if (tid < m) {                                       // entries differ: the place of one is the number of smaller ones
-        const uint32_t e = list_b[tid];
-        uint32_t rank = 0;
-        int j = 0;
-#pragma unroll 4
-        for (; j + 4 <= m; j += 4) {
-          const uint4 o = *reinterpret_cast<const uint4*>(list_b + j);
-          rank += (uint32_t)(o.x < e) + (uint32_t)(o.y < e) + (uint32_t)(o.z < e) + (uint32_t)(o.w < e);
-        }
-        for (; j < m; ++j) rank += (uint32_t)(list_b[j] < e);
-        list_a[rank] = e;
-      }
-      key = list_a;
+    // ---- a stable sort by row.  One token often makes up most of a long list (padding, the most frequent token): its entries go
+    // behind the others in one pass, and what is left is short.
+    uint32_t *key = list_b, *other = list_a;
+    int cold = m;                                          // entries that precede those of such a token
+    const int part = (m + ES_THREADS - 1) / ES_THREADS * 64, e0 = min(m, wave * part), e1 = min(m, e0 + part);     // a wave's
+    if (m > ES_RANK) {
+      const uint32_t sample = key[(long)lane * m / 64] >> p.n_bits;
+      const uint32_t votes = (uint32_t)__popcll(es_peers(sample, p.row_bits, ~0ull)) << 6 | (uint32_t)lane;
+      uint32_t best = votes;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o, 64));
+      const uint32_t hot = (uint32_t)__shfl((int)sample, (int)(best & 63), 64);
+      int mine_cold = 0;
+      for (int i = e0; i < e1; i += 64) mine_cold += (int)__popcll(__ballot(i + lane < e1 && key[i + lane] >> p.n_bits != hot));
+      if (lane == 0) bins[wave] = (uint32_t)mine_cold;
       __syncthreads();
-    } else if (m > ES_RANK) {
+      int to_cold = 0, all_cold = 0;
+#pragma unroll
+      for (int w = 0; w < ES_WAVES; ++w) {
+        to_cold += w < wave ? (int)bins[w] : 0;
+        all_cold += (int)bins[w];
+      }
+      if (all_cold <= ES_RANK) {
+        cold = all_cold;
+        int to_hot = cold + e0 - to_cold;
+        for (int i = e0; i < e1; i += 64) {
+          const bool on = i + lane < e1;
+          const uint32_t e = on ? key[i + lane] : 0;
+          const bool is_cold = e >> p.n_bits != hot;
+          const uint64_t cs = __ballot(on && is_cold), hs = __ballot(on && !is_cold);
+          if (on) other[is_cold ? to_cold + es_below(cs) : to_hot + es_below(hs)] = e;
+          to_cold += (int)__popcll(cs);
+          to_hot += (int)__popcll(hs);
+        }
+        uint32_t* t = key; key = other; other = t;
+      }
+      __syncthreads();
+    }
+    if (cold > 1 && cold <= ES_RANK) {
+      if (cold <= ES_COUNT) {                              // the place of an entry is the number of smaller ones: no two are equal
+        if (tid < cold) {
+          const uint32_t e = key[tid];
+          uint32_t rank = 0;
+          for (int j = 0; j < cold; j += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(key + j);
+            rank += (uint32_t)(o.x < e) + (uint32_t)(j + 1 < cold && o.y < e) + (uint32_t)(j + 2 < cold && o.z < e) + (uint32_t)(j + 3 < cold && o.w < e);
+          }
+          other[rank] = e;
+        }
+      } else {
+        // Each wave sorts 64 entries in registers, and the place of one is the number of smaller ones in all sorted runs.
+        uint32_t e = tid < cold ? key[tid] : ~0u;
+        for (int k2 = 2; k2 <= 64; k2 *= 2)
+          for (int o = k2 / 2; o > 0; o /= 2) {
+            const uint32_t y = (uint32_t)__shfl_xor((int)e, o, 64);
+            const bool up = (lane & k2) == 0, low = (lane & o) == 0;
+            e = up == low ? min(e, y) : max(e, y);
+          }
+        hist_or_heads[tid] = e;
+        __syncthreads();
+        if (tid - lane < cold && e != ~0u) {
+          uint32_t rank = 0;
+          for (int w = 0; w < (cold + 63) / 64; w += 4) {    // runs behind the last hold ~0
+            const uint32_t* run = hist_or_heads + w * 64;
+            uint32_t at[4] = {};
+#pragma unroll
+            for (int o = 32; o > 0; o /= 2)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) at[r] += run[r * 64 + at[r] + o - 1] < e ? o : 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) rank += at[r] + (uint32_t)(run[r * 64 + at[r]] < e);
+          }
+          other[rank] = e;
+        }
+      }
+      for (int i = cold + tid; i < m; i += ES_THREADS) other[i] = key[i];
+      key = other;
+      __syncthreads();
+    } else if (cold > ES_RANK) {
       uint32_t* hist = hist_or_heads + wave * ES_BINS;     // [wave][bin]
-      const int per = (m + ES_THREADS - 1) / ES_THREADS * 64, e0 = min(m, wave * per), e1 = min(m, e0 + per);
-      uint32_t *from = list_b, *to = list_a;
+      uint32_t *from = key, *to = other;
       const int passes = (max(1, p.row_bits) + ES_BITS - 1) / ES_BITS, digit = (max(1, p.row_bits) + passes - 1) / passes;
       for (int shift = p.n_bits; shift < p.n_bits + max(1, p.row_bits); shift += digit) {
         const uint32_t mask = (1u << digit) - 1;
@@ -172,7 +243,7 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
           const bool on = i + lane < e1;
           const uint32_t bin = on ? (from[i + lane] >> shift) & mask : 0;
           const uint64_t peers = es_peers(bin, digit, __ballot(on));
-          if (on && !(peers & below)) hist[bin] += (uint32_t)__popcll(peers);
+          if (on && es_below(peers) == 0) hist[bin] += (uint32_t)__popcll(peers);
           __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -204,10 +275,10 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
           uint32_t place = 0;
           if (on) {
             place = hist[bin];
-            to[place + (uint32_t)__popcll(peers & below)] = e;
+            to[place + es_below(peers)] = e;
           }
           __builtin_amdgcn_wave_barrier();
-          if (on && !(peers & below)) hist[bin] = place + (uint32_t)__popcll(peers);
+          if (on && es_below(peers) == 0) hist[bin] = place + (uint32_t)__popcll(peers);
           __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -217,11 +288,18 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
     }
     // ---- sums: a team takes an equal piece of the sorted list
     float* heads = reinterpret_cast<float*>(hist_or_heads);    // [team][W]: a team's part of a sum that an earlier team owns
-    const int per = (m + ES_TEAMS - 1) / ES_TEAMS, s = min(m, team * per), e = min(m, s + per);
+    // (with whole waves for the entries that are likely to be sums by themselves, each with a matrix row to read or write, and for the
+    // rest: teams of one wave that do different things wait for each other)
+    const int dear = cold < m ? cold : 0;
+    const int dear_teams = dear ? 64 / STRIP_LANES * max(1, min(ES_WAVES - 1, (ES_WAVES * ES_COLD_COST * dear + m / 2) / (m + (ES_COLD_COST - 1) * dear))) : 0;
+    const bool is_dear = team < dear_teams;
+    const int p0 = is_dear ? 0 : dear, p1 = is_dear ? dear : m, nth = is_dear ? team : team - dear_teams, of = is_dear ? dear_teams : ES_TEAMS - dear_teams;
+    const int per = (p1 - p0 + of - 1) / of, s = min(p1, p0 + nth * per), e = min(p1, s + per);
     const uint32_t mask_n = (1u << p.n_bits) - 1;
     float acc[P] = {}, old[P] = {};                        // of the sum under way; what the matrix holds
     auto place = [&](uint32_t r) __attribute__((always_inline)) { return p.dV + ((size_t)r << p.log2R | mine) * p.ldv + own.col; };
     auto write = [&](uint32_t r) __attribute__((always_inline)) {
+      if (!ADD && !first && (seen[r >> 5] >> (r & 31) & 1)) load_columns<float, P, WHOLE>(place(r), old, own.n);
 #pragma unroll
       for (int j = 0; j < P; ++j) old[j] = fmaf(p.scale, acc[j], old[j]);
       store_columns<float, P, WHOLE>(place(r), old, own.n);
@@ -231,12 +309,22 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
     if (s < e) {
       const T* dh = reinterpret_cast<const T*>(p.dh) + n_base * p.lddh + own.col;
       cur = key[s] >> p.n_bits;
-      bool head = s > 0 && key[s - 1] >> p.n_bits == cur;
+      bool head = s > p0 && key[s - 1] >> p.n_bits == cur;
       uint32_t before = head ? cur : ~0u;                  // row of the entry before the ones requested
-      constexpr int U = 4;                                 // rows requested together, with the matrix rows of sums that begin
+      constexpr int U = ADD && P == 8 ? 4 : 8;             // rows requested together (within 128 registers), with the matrix rows of sums that begin
       for (int i = s; i < e; i += U) {
         UnalignedPack<T, P> x[U] = {};
-        UnalignedPack<float, P> had[U] = {};
+        if (i > s && i + U <= e && key[i + U - 1] >> p.n_bits == cur) {      // the sum under way goes on: nothing but loads and additions
+#pragma unroll
+          for (int u = 0; u < U; ++u) load_raw_columns<T, P, WHOLE>(dh + (size_t)(key[i + u] & mask_n) * p.lddh, x[u], own.n);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < P; ++j) acc[j] += to_f32(x[u].v[j]);
+          before = cur;
+          continue;
+        }
+        UnalignedPack<float, P> had[ADD ? U : 1] = {};
         uint32_t r[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -244,7 +332,7 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
           r[u] = entry >> p.n_bits;
           if (i + u < e) {
             load_raw_columns<T, P, WHOLE>(dh + (size_t)(entry & mask_n) * p.lddh, x[u], own.n);
-            if (r[u] != before && (!overwrite || (!first && (seen[r[u] >> 5] >> (r[u] & 31) & 1)))) load_raw_columns<float, P, WHOLE>(place(r[u]), had[u], own.n);
+            if (ADD && r[u] != before) load_raw_columns<float, P, WHOLE>(place(r[u]), had[ADD ? u : 0], own.n);
           }
           before = r[u];
         }
@@ -264,13 +352,13 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
             }
             if (change || (i + u == s && !head)) {
 #pragma unroll
-              for (int j = 0; j < P; ++j) { acc[j] = 0.f; old[j] = had[u].v[j]; }
+              for (int j = 0; j < P; ++j) { acc[j] = 0.f; old[j] = ADD ? had[ADD ? u : 0].v[j] : 0.f; }
             }
 #pragma unroll
             for (int j = 0; j < P; ++j) acc[j] += to_f32(x[u].v[j]);
           }
       }
-      const bool goes_on = e < m && key[e] >> p.n_bits == cur;
+      const bool goes_on = e < p1 && key[e] >> p.n_bits == cur;
       pending = goes_on && !head;
       middle = goes_on && head;
       if (head) {
@@ -325,13 +413,16 @@ hipError_t launch_embed_bwd_sorted(hipStream_t s, int dtype, const int32_t* tok,
   const long long blocks = ((long long)p.slices << p.log2R) + p.clearers;
   if (blocks * ES_THREADS >> 32) return hipErrorInvalidValue;
   dim3 grid((unsigned)blocks), block(ES_THREADS);
-  if (dtype == 1) {
-    if (d >= 8) hipLaunchKernelGGL((embed_bwd_sorted_kernel<bf16_t, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((embed_bwd_sorted_kernel<bf16_t, false>), grid, block, 0, s, p);
-  } else {
-    if (d >= 4) hipLaunchKernelGGL((embed_bwd_sorted_kernel<float, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((embed_bwd_sorted_kernel<float, false>), grid, block, 0, s, p);
-  }
+#define OURO_LAUNCH(T_, WHOLE_)                                                                                              \
+  do {                                                                                                                       \
+    if (accumulate) hipLaunchKernelGGL((embed_bwd_sorted_kernel<T_, WHOLE_, true>), grid, block, 0, s, p);                   \
+    else hipLaunchKernelGGL((embed_bwd_sorted_kernel<T_, WHOLE_, false>), grid, block, 0, s, p);                             \
+  } while (0)
+  if (dtype == 1 && d >= 8) OURO_LAUNCH(bf16_t, true);
+  else if (dtype == 1) OURO_LAUNCH(bf16_t, false);
+  else if (d >= 4) OURO_LAUNCH(float, true);
+  else OURO_LAUNCH(float, false);
+#undef OURO_LAUNCH
   return hipGetLastError();
 }
 
