@@ -9,22 +9,26 @@
 // 2.6e-7, 1.7e-7).  All entries of X, A and the polynomial are below 5 in magnitude (|X|_2 <= 1.2); they are stored times 2^12, so that
 // the low halves of ordinary entries (1 / sqrt(rows cols)) stay above fp16's smallest normal number.
 //
-// All three products are of the form A B^T with the contraction contiguous in both: X X^T; the square of the symmetric A; and
-// (the polynomial, symmetric) times X^T, for which X is kept in both layouts.  Of the two symmetric results only the
-// tiles on and below the diagonal are formed and stored twice.  Matrices are the smaller dimension times the larger, padded with zeros
-// to whole multiples of 64: zero rows and columns stay zero in every step.
-#include "common.h"
+// With C = a I + b A + c A^2 a step is X <- C X, and the A of the step after it is C A C: all of these are polynomials of one symmetric
+// matrix, symmetric and commuting.  Two steps therefore need X only once: A = X X^T, C, (C A) C = A', C', C' C, X <- (C' C) X.  For
+// matrices twice as wide as high and more that is a quarter to a third less work, and X is written half as often (1024 x 4096: two steps
+// 2.0 -> 1.4 ms).  It is as accurate: errors of A' are absolute, 2^-22 |A|, and reach X through C' as 1e-6 of a.  Three steps without X
+// would not be: negative rounding noise in the small eigenvalues of A grows by a^2 a step.
+//
+// All products are of the form L R^T with the contraction contiguous in both: X X^T; products of two of the symmetric matrices; and one of
+// those times X^T, for which X is kept in both layouts.  Of the symmetric results only the tiles on and below the diagonal are formed, and
+// stored twice.  Matrices are the smaller dimension times the larger, padded with zeros to whole multiples of 64: zero rows and columns
+// stay zero in every step.
+#include "gemm_pp.h"
 #include "unaligned.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ouro {
 
 typedef _Float16 half_t;
-typedef __attribute__((ext_vector_type(4))) _Float16 half4;
-typedef __attribute__((ext_vector_type(8))) _Float16 half8;
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((address_space(3))) void ns_lds_void;
+typedef f16x8 half8;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float NS_SCALE = 4096.f, NS_DOWN = 1.f / 4096.f;
@@ -49,7 +53,7 @@ struct NsParams {
   float scale, eps;
   int parts;
   double* sums;                                            // [batch][parts]
-  char *x, *xt[2], *gram, *poly;                           // split matrices, batch after batch
+  char *x, *xt[2], *gram, *c, *t;                          // split matrices, batch after batch
 };
 
 // ------------------------------------------------------------------------- norm, momentum
@@ -59,22 +63,50 @@ __device__ __forceinline__ float ns_update(const NsParams& p, float g, float mom
 // Momentum, and the sum of squares in 64 bits: no gradient is too large or too small for it.
 template <typename T>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsParams p) {
+  constexpr int P = 16 / sizeof(T);
   __shared__ double part[4];
-  const int b = blockIdx.y;
+  const int b = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const T* g = reinterpret_cast<const T*>(p.g) + b * p.sg;
   float* mom = p.mom ? p.mom + b * p.sg : nullptr;
   double sum = 0;
-  for (int r = blockIdx.x; r < p.rows; r += p.parts)
-    for (int c = threadIdx.x; c < p.cols; c += 256) {
-      const size_t at = r * p.ldg + c;
-      const float x = to_f32(g[at]);
-      float m = 0.f;
-      if (mom) mom[at] = m = fmaf(p.mu, mom[at], x);
-      const double u = ns_update(p, x, m);
-      sum += u * u;
+  auto one = [&](size_t at, float x) __attribute__((always_inline)) {
+    float m = 0.f;
+    if (mom) mom[at] = m = fmaf(p.mu, mom[at], x);
+    const double u = ns_update(p, x, m);
+    sum += u * u;
+  };
+  for (int r = blockIdx.x * 4 + wave; r < p.rows; r += p.parts * 4) {
+    const size_t row = r * p.ldg;
+    const int whole = p.cols / P * P;
+#pragma unroll 2
+    for (int c = lane * P; c < whole; c += 64 * P) {
+      T x[P];
+      load_unaligned<T, P>(g + row + c, x);
+      if (mom) {
+#pragma unroll
+        for (int h = 0; h < P; h += 4) {
+          float m[4];
+          load_unaligned<float, 4>(mom + row + c + h, m);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            m[e] = fmaf(p.mu, m[e], to_f32(x[h + e]));
+            const double u = ns_update(p, to_f32(x[h + e]), m[e]);
+            sum += u * u;
+          }
+          store_unaligned<float, 4>(mom + row + c + h, m);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const double u = to_f32(x[e]);
+          sum += u * u;
+        }
+      }
     }
+    if (whole + lane < p.cols) one(row + whole + lane, to_f32(g[row + whole + lane]));
+  }
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  if (lane == 0) part[wave] = sum;
   __syncthreads();
   if (threadIdx.x == 0) p.sums[(size_t)b * p.parts + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
@@ -82,27 +114,52 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsParams p) {
 // X and its transpose, split and padded, from 64 x 64 tiles.
 template <typename T>
 __global__ __launch_bounds__(256) void ns_start_kernel(NsParams p) {
+  constexpr int P = 16 / sizeof(T);
   __shared__ float tile[64][65];
   __shared__ double part[4];
   const int tid = threadIdx.x, b = blockIdx.y, tiles_n = p.np / 64;
   const int r0 = blockIdx.x / tiles_n * 64, c0 = blockIdx.x % tiles_n * 64;    // of X
+  const T* g = reinterpret_cast<const T*>(p.g) + b * p.sg;
+  const float* mom = p.mom ? p.mom + b * p.sg : nullptr;
+  const int i0 = p.tall ? c0 : r0, j0 = p.tall ? r0 : c0;                      // of the caller's matrix
+  float u[16 / P][P];
+#pragma unroll
+  for (int k = 0; k < 16 / P; ++k) {
+    const int at = tid + 256 * k, i = i0 + at / (64 / P), j = j0 + at % (64 / P) * P;
+    T x[P] = {};
+    float m[P] = {};
+    if (i < p.rows) {
+      if (j + P <= p.cols) {
+        load_unaligned<T, P>(g + i * p.ldg + j, x);
+        if (mom)
+#pragma unroll
+          for (int h = 0; h < P; h += 4) load_unaligned<float, 4>(mom + i * p.ldg + j + h, m + h);
+      } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+          if (j + e < p.cols) {
+            x[e] = g[i * p.ldg + j + e];
+            if (mom) m[e] = mom[i * p.ldg + j + e];
+          }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < P; ++e) u[k][e] = ns_update(p, to_f32(x[e]), m[e]);
+  }
   double sum = tid < p.parts ? p.sums[(size_t)b * p.parts + tid] : 0;
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((tid & 63) == 0) part[tid >> 6] = sum;
   __syncthreads();
   const double inv = NS_SCALE / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + p.eps);    // in 64 bits as the sum
-  const T* g = reinterpret_cast<const T*>(p.g) + b * p.sg;
-  const float* mom = p.mom ? p.mom + b * p.sg : nullptr;
-  const int i0 = p.tall ? c0 : r0, j0 = p.tall ? r0 : c0;                      // of the caller's matrix
-  for (int k = tid; k < 64 * 64; k += 256) {
-    const int i = k >> 6, j = k & 63;
-    float u = 0.f;
-    if (i0 + i < p.rows && j0 + j < p.cols) {
-      const size_t at = (i0 + i) * p.ldg + j0 + j;
-      u = (float)(ns_update(p, to_f32(g[at]), mom ? mom[at] : 0.f) * inv);
+#pragma unroll
+  for (int k = 0; k < 16 / P; ++k) {
+    const int at = tid + 256 * k, i = at / (64 / P), j = at % (64 / P) * P;
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      const float x = (float)(u[k][e] * inv);
+      if (p.tall) tile[j + e][i] = x;
+      else tile[i][j + e] = x;
     }
-    if (p.tall) tile[j][i] = u;
-    else tile[i][j] = u;
   }
   __syncthreads();
   const size_t bytes = (size_t)p.mp * p.np * 4;
@@ -127,136 +184,270 @@ __global__ __launch_bounds__(256) void ns_start_kernel(NsParams p) {
 }
 
 // ------------------------------------------------------------------------------- products
-enum { NS_GRAM = 0, NS_POLY = 1, NS_NEXT = 2, NS_LAST = 3 };
+enum { NS_PLAIN = 0, NS_POLY = 1, NS_NEXT = 2, NS_LAST = 3 };     // L R^T (symmetric); a I + b L + c L L^T; X and X^T; the result
 struct NsProduct {
   const char* a; const char* b;                            // split [rows_a][32 k_tiles], [rows_b][32 k_tiles], batch after batch
   int rows_a, rows_b, k_tiles;
   int tiles_b;                                             // tiles along rows_b; symmetric results: 0
   int tiles;                                               // of one matrix
-  const char* xt;                                          // NEXT, LAST: X^T
-  char* out; char* out_t;                                  // GRAM, POLY: the result; NEXT: X and X^T
+  char* out; char* out_t;                                  // PLAIN, POLY: the result; NEXT: X and X^T
 };
 
-__device__ __forceinline__ void ns_request(const void* base, int bytes, char* dst, uint32_t voff, uint32_t k) {
-  auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (ns_lds_void*)dst, 16, voff, k, 0, 0);
+// The matrix and the tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn; an XCD takes a run of neighbouring tiles, whose
+// operands its L2 then shares.
+struct NsTile { int b, ti, tj; };
+__device__ __forceinline__ NsTile ns_tile(const NsProduct& q) {
+  const int nb = gridDim.x, share = nb >> 3, rest = nb & 7, xcd = blockIdx.x & 7, bid = xcd * share + min(xcd, rest) + (blockIdx.x >> 3);
+  NsTile r;
+  r.b = bid / q.tiles;
+  const int t = bid - r.b * q.tiles;
+  if (q.tiles_b) {
+    r.ti = t / q.tiles_b;
+    r.tj = t - r.ti * q.tiles_b;
+  } else {                                                 // row ti of the triangle begins at ti (ti + 1) / 2
+    r.ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+    while (r.ti * (r.ti + 1) / 2 > t) --r.ti;
+    while ((r.ti + 1) * (r.ti + 2) / 2 <= t) ++r.ti;
+    r.tj = t - r.ti * (r.ti + 1) / 2;
+  }
+  return r;
 }
 
-// 64 S x 64 S tiles, four waves of 32 S x 32 S each.  A K-tile is 32 of the contraction: 128-byte rows of high and low halves in LDS, two
-// stages, 16-byte chunk c of a row at c ^ swizzle(row).
-template <int S, int KIND, typename T>
-__global__ __launch_bounds__(256) void ns_product_kernel(NsParams p, NsProduct q) {
-  constexpr int ROWS = 64 * S, STAGE = 2 * ROWS * 128;
-  extern __shared__ char ns_lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = blockIdx.x / q.tiles, t = blockIdx.x - b * q.tiles;
-  int ti, tj;
-  if (q.tiles_b) { ti = t / q.tiles_b; tj = t - ti * q.tiles_b; }
-  else {                                                   // row ti of the triangle begins at ti (ti + 1) / 2
-    ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-    while (ti * (ti + 1) / 2 > t) --ti;
-    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-    tj = t - ti * (ti + 1) / 2;
-  }
-  const int m0 = ti * ROWS, n0 = tj * ROWS, ld = q.k_tiles * 128;
-  const int bytes_a = q.rows_a * ld, bytes_b = q.rows_b * ld;
-  const char* A = q.a + (size_t)b * bytes_a;
-  const char* B = q.b + (size_t)b * bytes_b;
-  auto swizzle = [](int row) { return (row ^ (row >> 3)) & 7; };
-  auto request = [&](int kt) __attribute__((always_inline)) {
-    char* dst = ns_lds + (kt & 1) * STAGE;
+// One 32 x 32 piece of a product at (m, n) of matrix b.  In both layouts its rows are full 128-byte lines (32 high halves, 32 low ones).
+// The accumulators go through the wave's patch of LDS, [n][m] as lanes hold them, and leave first with m contiguous (where
+// what is added comes from), then with n contiguous.
+constexpr int NS_PATCH = 32 * 36;                          // floats
+template <int KIND, typename T>
+__device__ __forceinline__ void ns_epilogue(const NsParams& p, const NsProduct& q, int b, int m, int n, bool diagonal, const f32x16& acc, float* patch, int lane) {
+  if (m >= q.rows_a || n >= q.rows_b) return;              // both are multiples of 64
+  const size_t mat = (size_t)b * q.rows_a * q.rows_b * 4;
+  const int row = lane >> 2, c = (lane & 3) * 8;
+  half8 old_hi[2], old_lo[2];
+  if (KIND == NS_POLY) {                                   // A itself, symmetric
 #pragma unroll
-    for (int i = 0; i < 2 * S; ++i) {                      // 8 rows a request
-      const int row = (wave * 2 * S + i) * 8 + (lane >> 3);
-      const uint32_t off = (uint32_t)(((lane & 7) ^ swizzle(row)) << 4);
-      ns_request(A, bytes_a, dst + (wave * 2 * S + i) * 1024, (uint32_t)(m0 + row) * ld + off, kt * 128);
-      ns_request(B, bytes_b, dst + ROWS * 128 + (wave * 2 * S + i) * 1024, (uint32_t)(n0 + row) * ld + off, kt * 128);
+    for (int it = 0; it < 2; ++it) {
+      const char* old = q.a + mat + ns_at(n + 16 * it + row, m + c, q.rows_a);
+      old_hi[it] = *reinterpret_cast<const half8*>(old);
+      old_lo[it] = *reinterpret_cast<const half8*>(old + 64);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    *reinterpret_cast<float4*>(patch + (lane & 31) * 36 + 8 * r + 4 * (lane >> 5)) =
+        make_float4(acc[4 * r] * NS_DOWN, acc[4 * r + 1] * NS_DOWN, acc[4 * r + 2] * NS_DOWN, acc[4 * r + 3] * NS_DOWN);
+  __builtin_amdgcn_wave_barrier();
+  auto store_split = [](char* at, const float* v) __attribute__((always_inline)) {
+    half8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      half_t h, l;
+      ns_split(v[e], h, l);
+      hi[e] = h; lo[e] = l;
+    }
+    *reinterpret_cast<half8*>(at) = hi;
+    *reinterpret_cast<half8*>(at + 64) = lo;
+  };
+  auto store_result = [&](int i, int j, int lim_i, int lim_j, const float* v) __attribute__((always_inline)) {     // o[i][j ...]
+    if (i >= lim_i) return;
+    T* o = reinterpret_cast<T*>(p.o) + b * p.so + i * p.ldo + j;
+    T w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = from_f32<T>(v[e] * (p.scale * NS_DOWN));
+    if (j + 8 <= lim_j) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 16 / (int)sizeof(T)) store_unaligned<T, 16 / sizeof(T)>(o + e, w + e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (j + e < lim_j) o[e] = w[e];
     }
   };
-  f32x16_t acc[S][S];
 #pragma unroll
-  for (int i = 0; i < S; ++i)
+  for (int it = 0; it < 2; ++it) {
+    float* at = patch + (16 * it + row) * 36 + c;
+    float v[8];
+    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(at);
+    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(at + 4);
+    if (KIND == NS_POLY) {
 #pragma unroll
-    for (int j = 0; j < S; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  const int wm = (wave >> 1) * 32 * S, wn = (wave & 1) * 32 * S;
-  request(0);
-  for (int kt = 0; kt < q.k_tiles; ++kt) {
-    __syncthreads();                                       // K-tile kt has arrived, and nobody reads the other stage
-    if (kt + 1 < q.k_tiles) request(kt + 1);
-    const char* st = ns_lds + (kt & 1) * STAGE;
-    half8 fa[S][4], fb[S][4];                              // chunks: high 0-15, high 16-31, low 0-15, low 16-31
-#pragma unroll
-    for (int i = 0; i < S; ++i)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int ra = wm + 32 * i + (lane & 31), rb = wn + 32 * i + (lane & 31), ch = 2 * c + (lane >> 5);
-        fa[i][c] = *reinterpret_cast<const half8*>(st + ra * 128 + ((ch ^ swizzle(ra)) << 4));
-        fb[i][c] = *reinterpret_cast<const half8*>(st + ROWS * 128 + rb * 128 + ((ch ^ swizzle(rb)) << 4));
+      for (int e = 0; e < 8; ++e) {
+        const float x = (float)old_hi[it][e] + (float)old_lo[it][e];
+        v[e] = fmaf(NS_C, v[e], fmaf(NS_B, x, m + c + e == n + 16 * it + row ? NS_A * NS_SCALE : 0.f));
       }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int i = 0; i < S; ++i)
-#pragma unroll
-        for (int j = 0; j < S; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[i][ks], fb[j][ks], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[i][ks], fb[j][2 + ks], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[i][2 + ks], fb[j][ks], acc[i][j], 0, 0, 0);
-        }
+      *reinterpret_cast<float4*>(at) = *reinterpret_cast<const float4*>(v);
+      *reinterpret_cast<float4*>(at + 4) = *reinterpret_cast<const float4*>(v + 4);
+    }
+    if (KIND == NS_LAST) {
+      if (p.tall) store_result(n + 16 * it + row, m + c, p.n, p.m, v);
+    } else {
+      store_split((KIND == NS_NEXT ? q.out_t : q.out) + mat + ns_at(n + 16 * it + row, m + c, q.rows_a), v);
+    }
   }
-  // ---- epilogue: a lane holds four neighbouring rows (m) of one column (n)
-  const int cols_t = q.rows_a;                             // row length of what is stored with m contiguous
-  const size_t mat = (size_t)b * q.rows_a * q.rows_b * 4;
+  __builtin_amdgcn_wave_barrier();
+  if (KIND == NS_LAST ? !p.tall : KIND == NS_NEXT || !diagonal) {      // a tile on the diagonal holds both of each pair
 #pragma unroll
-  for (int i = 0; i < S; ++i)
+    for (int it = 0; it < 2; ++it) {
+      float v[8];
 #pragma unroll
-    for (int j = 0; j < S; ++j) {
-      const int n = n0 + wn + 32 * j + (lane & 31);
+      for (int e = 0; e < 8; ++e) v[e] = patch[(c + e) * 36 + 16 * it + row];
+      if (KIND == NS_LAST) store_result(m + 16 * it + row, n + c, p.m, p.n, v);
+      else store_split(q.out + mat + ns_at(m + 16 * it + row, n + c, q.rows_b), v);
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The fragments of a K-tile, S 32-row tiles of either operand, four chunks (high 0-15, high 16-31, low 0-15, low 16-31) each.  One block of
+// assembly, with its wait: the compiler cannot tell an LDS read from the target of the direct loads in flight and would drain
+// those first.
+__device__ __forceinline__ void ns_read(half8 (&a)[1][4], half8 (&b)[1][4], const uint32_t* ra, const uint32_t* rb) {
+  asm volatile(
+      "ds_read_b128 %0, %8\n\tds_read_b128 %4, %12\n\tds_read_b128 %1, %9\n\tds_read_b128 %5, %13\n\t"
+      "ds_read_b128 %2, %10\n\tds_read_b128 %6, %14\n\tds_read_b128 %3, %11\n\tds_read_b128 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(a[0][0]), "=&v"(a[0][1]), "=&v"(a[0][2]), "=&v"(a[0][3]), "=&v"(b[0][0]), "=&v"(b[0][1]), "=&v"(b[0][2]), "=&v"(b[0][3])
+      : "v"(ra[0]), "v"(ra[1]), "v"(ra[2]), "v"(ra[3]), "v"(rb[0]), "v"(rb[1]), "v"(rb[2]), "v"(rb[3])
+      : "memory");
+}
+__device__ __forceinline__ void ns_read(half8 (&a)[2][4], half8 (&b)[2][4], const uint32_t* ra, const uint32_t* rb) {
+  asm volatile(
+      "ds_read_b128 %0, %16\n\tds_read_b128 %4, %16 offset:4096\n\tds_read_b128 %8, %20\n\tds_read_b128 %12, %20 offset:4096\n\t"
+      "ds_read_b128 %1, %17\n\tds_read_b128 %5, %17 offset:4096\n\tds_read_b128 %9, %21\n\tds_read_b128 %13, %21 offset:4096\n\t"
+      "ds_read_b128 %2, %18\n\tds_read_b128 %6, %18 offset:4096\n\tds_read_b128 %10, %22\n\tds_read_b128 %14, %22 offset:4096\n\t"
+      "ds_read_b128 %3, %19\n\tds_read_b128 %7, %19 offset:4096\n\tds_read_b128 %11, %23\n\tds_read_b128 %15, %23 offset:4096\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(a[0][0]), "=&v"(a[0][1]), "=&v"(a[0][2]), "=&v"(a[0][3]), "=&v"(a[1][0]), "=&v"(a[1][1]), "=&v"(a[1][2]), "=&v"(a[1][3]),
+        "=&v"(b[0][0]), "=&v"(b[0][1]), "=&v"(b[0][2]), "=&v"(b[0][3]), "=&v"(b[1][0]), "=&v"(b[1][1]), "=&v"(b[1][2]), "=&v"(b[1][3])
+      : "v"(ra[0]), "v"(ra[1]), "v"(ra[2]), "v"(ra[3]), "v"(rb[0]), "v"(rb[1]), "v"(rb[2]), "v"(rb[3])
+      : "memory");
+}
+
+__device__ __forceinline__ void ns_request(const char* base, int bytes, char* dst, uint32_t voff, uint32_t k) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000), (lds_void*)dst, 16, voff, k, 0, 0);
+}
+
+// 64 S x 64 S tiles, four waves of 32 S x 32 S each.  A K-tile is 32 of the contraction: 128-byte rows of high and low halves in LDS, 16-byte
+// chunk c of a row at c ^ swizzle(row), in a ring of D stages filled by direct loads that stay in flight over the barriers.  G groups
+// of four waves take every G-th K-tile each and are added up in order at the end: with one workgroup a CU a K-tile costs its latency
+// (wait, barrier, fragments, six dependent matrix instructions: 0.37 us), and four at a time a quarter of it.
+template <int S, int G> struct NsSmall {
+  static constexpr int ROWS = 64 * S, STAGE = 2 * ROWS * 128, D = S == 1 && G == 1 ? 4 : 2, LDS = G * D * STAGE;
+};
+template <int S, int G, int KIND, typename T>
+__global__ __launch_bounds__(256 * G) void ns_product_kernel(NsParams p, NsProduct q) {
+  constexpr int ROWS = NsSmall<S, G>::ROWS, STAGE = NsSmall<S, G>::STAGE, D = NsSmall<S, G>::D, PER = 4 * S;
+  extern __shared__ uint4 smem[];
+  static_assert(NsSmall<S, G>::LDS >= (G - 1) * 4 * S * S * 4096 + 4 * NS_PATCH * 4, "the groups' sums and the epilogue's patches fit the ring");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3, group = __builtin_amdgcn_readfirstlane(tid >> 8);
+  char* const lds = reinterpret_cast<char*>(smem) + group * D * STAGE;
+  const NsTile t = ns_tile(q);
+  const int m0 = t.ti * ROWS, n0 = t.tj * ROWS, ld = q.k_tiles * 128;
+  const int bytes_a = q.rows_a * ld, bytes_b = q.rows_b * ld;
+  const char* A = q.a + (size_t)t.b * bytes_a;
+  const char* B = q.b + (size_t)t.b * bytes_b;
+  auto swizzle = [](int row) { return (row ^ ((row & 31) >> 3)) & 7; };
+  uint32_t oa[2 * S], ob[2 * S];                           // 8 rows a request; rows past the end read as zero
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int m = m0 + wm + 32 * i + 8 * r + 4 * (lane >> 5);
-        if (m >= q.rows_a || n >= q.rows_b) continue;
-        float v[4];
+  for (int i = 0; i < 2 * S; ++i) {
+    const int row = (wave * 2 * S + i) * 8 + (lane >> 3);
+    const uint32_t off = (uint32_t)(((lane & 7) ^ swizzle(row)) << 4);
+    oa[i] = (uint32_t)(m0 + row) * ld + off;
+    ob[i] = (uint32_t)(n0 + row) * ld + off;
+  }
+  const int mine = (q.k_tiles - group + G - 1) / G, most = (q.k_tiles + G - 1) / G;     // K-tiles group, group + G, ...
+  auto request = [&](int i, int stage) __attribute__((always_inline)) {
+    char* dst = lds + stage * STAGE + wave * 2 * S * 1024;
+    const uint32_t k = (uint32_t)(i * G + group) * 128;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * r + e] * NS_DOWN;
-        if (KIND != NS_GRAM) {
-          // POLY: A itself, symmetric; NEXT, LAST: X^T
-          const char* old = (KIND == NS_POLY ? q.a : q.xt) + mat + ns_at(n, m, cols_t);
-          const half4 hi = *reinterpret_cast<const half4*>(old), lo = *reinterpret_cast<const half4*>(old + 64);
+    for (int r = 0; r < 2 * S; ++r) {
+      ns_request(A, bytes_a, dst + r * 1024, oa[r], k);
+      ns_request(B, bytes_b, dst + ROWS * 128 + r * 1024, ob[r], k);
+    }
+  };
+  f32x16 acc[S][S];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = (float)hi[e] + (float)lo[e];
-            v[e] = KIND == NS_POLY ? fmaf(NS_C, v[e], NS_B * x) : fmaf(NS_A, x, v[e]);
-          }
-        }
-        if (KIND == NS_LAST) {
-          T* o = reinterpret_cast<T*>(p.o) + b * p.so;
+  for (int i = 0; i < S * S; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m + e < p.m && n < p.n) o[p.tall ? n * p.ldo + m + e : (m + e) * p.ldo + n] = from_f32<T>(v[e] * (p.scale * NS_DOWN));
-          continue;
-        }
-        half4 hi, lo;
+    for (int r = 0; r < 16; ++r) acc[i / S][i % S][r] = 0.f;
+  const int wm = (wave >> 1) * 32 * S, wn = (wave & 1) * 32 * S;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  uint32_t fa0[4], fb0[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          half_t h, l;
-          ns_split(v[e], h, l);
-          hi[e] = h; lo[e] = l;
-        }
-        char* at = (KIND == NS_NEXT ? q.out_t : q.out) + mat + ns_at(n, m, cols_t);
-        *reinterpret_cast<half4*>(at) = hi;
-        *reinterpret_cast<half4*>(at + 64) = lo;
-        if (KIND != NS_NEXT && ti == tj) continue;         // a tile on the diagonal holds both of each pair
+  for (int c = 0; c < 4; ++c) {
+    const int ra = wm + (lane & 31), rb = wn + (lane & 31), ch = 2 * c + (lane >> 5);
+    fa0[c] = lds0 + ra * 128 + ((ch ^ swizzle(ra)) << 4);
+    fb0[c] = lds0 + ROWS * 128 + rb * 128 + ((ch ^ swizzle(rb)) << 4);
+  }
+  for (int i = 0; i < D - 1 && i < mine; ++i) request(i, i);
+  int stage = 0;
+  for (int i = 0; i < most; ++i) {
+    if (i + D - 2 < mine) pp_wait_mem<PER*(D - 2)>();      // the group's K-tile i has arrived
+    else pp_wait_mem<0>();
+    pp_barrier();                                          // ... for every wave, and nobody reads the stage that is filled next
+    if (i + D - 1 < mine) request(i + D - 1, stage == 0 ? D - 1 : stage - 1);
+    if (i < mine) {
+      half8 fa[S][4], fb[S][4];
+      uint32_t ra[4], rb[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          char* d = q.out + mat + ns_at(m + e, n, q.rows_b);
-          *reinterpret_cast<half_t*>(d) = hi[e];
-          *reinterpret_cast<half_t*>(d + 64) = lo[e];
-        }
+      for (int c = 0; c < 4; ++c) { ra[c] = fa0[c] + stage * STAGE; rb[c] = fb0[c] + stage * STAGE; }
+      ns_read(fa, fb, ra, rb);
+#pragma unroll
+      for (int pass = 0; pass < 6; ++pass) {
+        const int ca = pass >> 1 == 2 ? 2 + (pass & 1) : pass & 1, cb = pass >> 1 == 1 ? 2 + (pass & 1) : pass & 1;
+#pragma unroll
+        for (int r = 0; r < S * S; ++r) acc[r / S][r % S] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r / S][ca], fb[r % S][cb], acc[r / S][r % S], 0, 0, 0);
       }
     }
+    stage = stage + 1 == D ? 0 : stage + 1;
+  }
+  __syncthreads();
+  if (G > 1) {
+    float4* sums = reinterpret_cast<float4*>(smem);        // [group - 1][wave][piece][4][lane]
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < S * S; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          sums[((((group - 1) * 4 + wave) * S * S + i) * 4 + r) * 64 + lane] =
+              make_float4(acc[i / S][i % S][4 * r], acc[i / S][i % S][4 * r + 1], acc[i / S][i % S][4 * r + 2], acc[i / S][i % S][4 * r + 3]);
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int g = 0; g < G - 1; ++g)
+#pragma unroll
+      for (int i = 0; i < S * S; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 v = sums[(((g * 4 + wave) * S * S + i) * 4 + r) * 64 + lane];
+          acc[i / S][i % S][4 * r] += v.x; acc[i / S][i % S][4 * r + 1] += v.y; acc[i / S][i % S][4 * r + 2] += v.z; acc[i / S][i % S][4 * r + 3] += v.w;
+        }
+  }
+  float* patch = reinterpret_cast<float*>(smem) + (G - 1) * 4 * S * S * 1024 + wave * NS_PATCH;      // behind the sums, which other waves may still read
+#pragma unroll
+  for (int i = 0; i < S * S; ++i)
+    ns_epilogue<KIND, T>(p, q, t.b, m0 + wm + 32 * (i / S), n0 + wn + 32 * (i % S), t.ti == t.tj, acc[i / S][i % S], patch, lane);
+}
+
+// 256 x 256 tiles (gemm_pp.h).
+template <int KIND, typename T>
+__global__ __launch_bounds__(512, 2) void ns_product_pp_kernel(NsParams p, NsProduct q) {
+  extern __shared__ uint4 smem[];
+  static_assert(PP_LDS >= 8 * NS_PATCH * 4, "the epilogue's patches fit the ring");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const NsTile t = ns_tile(q);
+  const int m0 = t.ti * 256, n0 = t.tj * 256;
+  GemmParams g;                                            // what the main loop reads of it
+  g.lda = g.ldb = q.k_tiles * 64;
+  g.bytesA = q.rows_a * q.k_tiles * 128;
+  g.bytesB = q.rows_b * q.k_tiles * 128;
+  g.A = q.a + (size_t)t.b * g.bytesA;
+  g.B = q.b + (size_t)t.b * g.bytesB;
+  f32x16 acc[4][2];
+  pp_mainloop<false, true, true>(g, m0, n0, 0, q.k_tiles, reinterpret_cast<char*>(smem), acc);
+  float* patch = reinterpret_cast<float*>(smem) + wave * NS_PATCH;
+  const int m_w = m0 + 64 * (wave >> 2), n_w = n0 + 32 * (wave & 3);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    ns_epilogue<KIND, T>(p, q, t.b, m_w + 128 * (i >> 2) + 32 * ((i >> 1) & 1), n_w + 128 * (i & 1), t.ti == t.tj, acc[i >> 1][i & 1], patch, lane);
 }
 
 // ---------------------------------------------------------------------------------- host
@@ -264,38 +455,76 @@ static int ns_pad(int x) { return (x + 63) / 64 * 64; }
 static size_t ns_align(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t orthogonalize_scratch_floats(int batch, int rows, int cols) {
   const size_t mp = ns_pad(std::min(rows, cols)), np = ns_pad(std::max(rows, cols));
-  return (ns_align((size_t)batch * NS_NORM_PARTS * 8) + (size_t)batch * 4 * (3 * mp * np + 2 * mp * mp)) / 4;
+  return (ns_align((size_t)batch * NS_NORM_PARTS * 8) + (size_t)batch * 4 * (3 * mp * np + 3 * mp * mp)) / 4;
 }
 
-template <int S, int KIND, typename T>
-static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int batch) {
-  constexpr int ROWS = 64 * S;
-  const int ta = (q.rows_a + ROWS - 1) / ROWS, tb = (q.rows_b + ROWS - 1) / ROWS;
-  const bool symmetric = KIND == NS_GRAM || KIND == NS_POLY;
-  q.tiles_b = symmetric ? 0 : tb;
-  q.tiles = symmetric ? ta * (ta + 1) / 2 : ta * tb;
-  hipLaunchKernelGGL((ns_product_kernel<S, KIND, T>), dim3((unsigned)(q.tiles * batch)), dim3(256), 2 * 2 * ROWS * 128, s, p, q);
+static long long ns_tiles(int edge, int rows_a, int rows_b, bool symmetric) {
+  const long long ta = (rows_a + edge - 1) / edge, tb = (rows_b + edge - 1) / edge;
+  return symmetric ? ta * (ta + 1) / 2 : ta * tb;
+}
+template <int S, int G, int KIND, typename T>
+static hipError_t ns_launch_small(hipStream_t s, dim3 grid, const NsParams& p, const NsProduct& q) {
+  static bool allowed = false;
+  hipError_t e = pp_allow_lds((const void*)ns_product_kernel<S, G, KIND, T>, NsSmall<S, G>::LDS, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((ns_product_kernel<S, G, KIND, T>), grid, dim3(256 * G), (NsSmall<S, G>::LDS), s, p, q);
   return hipGetLastError();
 }
+// One product of every matrix of the batch: 256 wide tiles where they fill the chip, else 128 wide ones, else 64; with few 64 wide tiles
+// the contraction is dealt to four groups of waves.
+template <int KIND, typename T>
+static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int batch) {
+  const bool symmetric = KIND == NS_PLAIN || KIND == NS_POLY;
+  int edge = 256;
+  while (edge > 64 && ns_tiles(edge, q.rows_a, q.rows_b, symmetric) * batch < 192) edge /= 2;
+  q.tiles = (int)ns_tiles(edge, q.rows_a, q.rows_b, symmetric);
+  q.tiles_b = symmetric ? 0 : (q.rows_b + edge - 1) / edge;
+  const dim3 grid((unsigned)(q.tiles * batch));
+  if (edge == 256) {
+    static bool allowed = false;
+    hipError_t e = pp_allow_lds((const void*)ns_product_pp_kernel<KIND, T>, PP_LDS, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((ns_product_pp_kernel<KIND, T>), grid, dim3(512), PP_LDS, s, p, q);
+    return hipGetLastError();
+  }
+  if (edge == 128) return ns_launch_small<2, 1, KIND, T>(s, grid, p, q);
+  return q.tiles * batch <= 256 && q.k_tiles >= 8 ? ns_launch_small<1, 4, KIND, T>(s, grid, p, q) : ns_launch_small<1, 1, KIND, T>(s, grid, p, q);
+}
 
-template <typename T, int S>
+template <typename T>
 static hipError_t ns_run(hipStream_t s, NsParams& p, int batch, int steps) {
   hipLaunchKernelGGL(ns_norm_kernel<T>, dim3(p.parts, batch), dim3(256), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(ns_start_kernel<T>, dim3(p.mp / 64 * (p.np / 64), batch), dim3(256), 0, s, p);
   e = hipGetLastError();
-  for (int i = 0; i < steps && e == hipSuccess; ++i) {
+  const bool pairs = p.np >= 2 * p.mp;                     // two steps with X once (see above); below, a pair is no less work
+  for (int i = 0, half = 0; i < steps && e == hipSuccess; half ^= 1) {
+    const bool two = pairs && i + 1 < steps;
+    auto product = [&](auto kind, const char* l, const char* r, int k_tiles, char* out) {
+      NsProduct q;
+      memset(&q, 0, sizeof q);
+      q.a = l; q.b = r; q.rows_a = q.rows_b = p.mp; q.k_tiles = k_tiles; q.out = out;
+      if (e == hipSuccess) e = ns_product<decltype(kind)::value, float>(s, p, q, batch);
+    };
+    constexpr std::integral_constant<int, NS_PLAIN> plain{};
+    constexpr std::integral_constant<int, NS_POLY> poly{};
+    product(plain, p.x, p.x, p.np / 32, p.gram);           // A
+    product(poly, p.gram, p.gram, p.mp / 32, p.c);         // C
+    const char* by = p.c;
+    if (two) {
+      product(plain, p.c, p.gram, p.mp / 32, p.t);         // C A
+      product(plain, p.t, p.c, p.mp / 32, p.gram);         // A' = C A C
+      product(poly, p.gram, p.gram, p.mp / 32, p.t);       // C'
+      product(plain, p.t, p.c, p.mp / 32, p.gram);         // C' C
+      by = p.gram;
+    }
+    i += two ? 2 : 1;
+    if (e != hipSuccess) break;
     NsProduct q;
     memset(&q, 0, sizeof q);
-    q.a = q.b = p.x; q.rows_a = q.rows_b = p.mp; q.k_tiles = p.np / 32; q.out = p.gram;
-    e = ns_product<S, NS_GRAM, float>(s, p, q, batch);
-    if (e != hipSuccess) break;
-    q.a = q.b = p.gram; q.k_tiles = p.mp / 32; q.out = p.poly;
-    e = ns_product<S, NS_POLY, float>(s, p, q, batch);
-    if (e != hipSuccess) break;
-    q.a = p.poly; q.b = q.xt = p.xt[i & 1]; q.rows_b = p.np; q.out = p.x; q.out_t = p.xt[1 - (i & 1)];
-    e = i + 1 < steps ? ns_product<S, NS_NEXT, float>(s, p, q, batch) : ns_product<S, NS_LAST, T>(s, p, q, batch);
+    q.a = by; q.b = p.xt[half]; q.rows_a = p.mp; q.rows_b = p.np; q.k_tiles = p.mp / 32; q.out = p.x; q.out_t = p.xt[1 - half];
+    e = i < steps ? ns_product<NS_NEXT, float>(s, p, q, batch) : ns_product<NS_LAST, T>(s, p, q, batch);
   }
   return e;
 }
@@ -307,7 +536,7 @@ hipError_t launch_orthogonalize(hipStream_t s, int dtype, const OrthogonalizeDes
   p.m = std::min(d.rows, d.cols); p.n = std::max(d.rows, d.cols); p.mp = ns_pad(p.m); p.np = ns_pad(p.n);
   p.g = d.g; p.ldg = d.ldg; p.sg = d.sg; p.mom = d.momentum; p.mu = d.mu; p.nesterov = d.nesterov;
   p.o = d.o; p.ldo = d.ldo; p.so = d.so; p.scale = d.scale; p.eps = d.eps;
-  p.parts = std::min({NS_NORM_PARTS, p.rows, std::max(16, 2048 / d.batch)});
+  p.parts = std::min({NS_NORM_PARTS, (p.rows + 3) / 4, std::max(16, 2048 / d.batch)});
   const size_t big = (size_t)d.batch * p.mp * p.np * 4, small = (size_t)d.batch * p.mp * p.mp * 4;
   char* at = reinterpret_cast<char*>(d.scratch);
   p.sums = reinterpret_cast<double*>(at); at += ns_align((size_t)d.batch * NS_NORM_PARTS * 8);
@@ -315,8 +544,9 @@ hipError_t launch_orthogonalize(hipStream_t s, int dtype, const OrthogonalizeDes
   p.xt[0] = at; at += big;
   p.xt[1] = at; at += big;
   p.gram = at; at += small;
-  p.poly = at;
-  return dtype == 1 ? ns_run<bf16_t, 1>(s, p, d.batch, d.steps) : ns_run<float, 1>(s, p, d.batch, d.steps);
+  p.c = at; at += small;
+  p.t = at;
+  return dtype == 1 ? ns_run<bf16_t>(s, p, d.batch, d.steps) : ns_run<float>(s, p, d.batch, d.steps);
 }
 
 }  // namespace ouro
