@@ -330,7 +330,7 @@ __device__ __forceinline__ void ns_request(const char* base, int bytes, char* ds
 // of four waves take every G-th K-tile each and are added up in order at the end: with one workgroup a CU a K-tile costs its latency
 // (wait, barrier, fragments, six dependent matrix instructions: 0.37 us), and four at a time a quarter of it.
 template <int S, int G> struct NsSmall {
-  static constexpr int ROWS = 64 * S, STAGE = 2 * ROWS * 128, D = S == 1 && G == 1 ? 4 : 2, LDS = G * D * STAGE;
+  static constexpr int ROWS = 64 * S, STAGE = 2 * ROWS * 128, D = 2, LDS = G * D * STAGE;
 };
 template <int S, int G, int KIND, typename T>
 __global__ __launch_bounds__(256 * G) void ns_product_kernel(NsParams p, NsProduct q) {
@@ -470,8 +470,9 @@ static hipError_t ns_launch_small(hipStream_t s, dim3 grid, const NsParams& p, c
   hipLaunchKernelGGL((ns_product_kernel<S, G, KIND, T>), grid, dim3(256 * G), (NsSmall<S, G>::LDS), s, p, q);
   return hipGetLastError();
 }
-// One product of every matrix of the batch: 256 wide tiles where they fill the chip, else 128 wide ones, else 64; with few 64 wide tiles
-// the contraction is dealt to four groups of waves.
+// One product of every matrix of the batch: 256 wide tiles where they fill the chip, else 128 wide ones, else 64; with 64 wide tiles
+// the contraction is dealt to four groups of waves where there is a workgroup a CU, else to two.  (One matrix of 1024 x 1024: four groups
+// 197 us, two 213, one 247; of 2048 x 2048: two 936, four 973, one 1060.)
 template <int KIND, typename T>
 static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int batch) {
   const bool symmetric = KIND == NS_PLAIN || KIND == NS_POLY;
@@ -488,7 +489,7 @@ static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int 
     return hipGetLastError();
   }
   if (edge == 128) return ns_launch_small<2, 1, KIND, T>(s, grid, p, q);
-  return q.tiles * batch <= 256 && q.k_tiles >= 8 ? ns_launch_small<1, 4, KIND, T>(s, grid, p, q) : ns_launch_small<1, 1, KIND, T>(s, grid, p, q);
+  return q.tiles * batch <= 256 && q.k_tiles >= 8 ? ns_launch_small<1, 4, KIND, T>(s, grid, p, q) : ns_launch_small<1, 2, KIND, T>(s, grid, p, q);
 }
 
 template <typename T>
