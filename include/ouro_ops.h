@@ -189,7 +189,8 @@ int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const 
  * read, h is zero there, and the state stays what it is.
  * states: fp32 [B, ceil(T / OURO_RECURRENCE_STRIDE), D] or NULL: the state that enters every OURO_RECURRENCE_STRIDE-th
  * step, which is what the backward call needs.
- * scratch: fp32, ouro_op_recurrence_scratch() floats (NULL where that is 0); a few long streams are cut into segments.
+ * scratch: fp32, ouro_op_recurrence_scratch() floats, 16-byte aligned (NULL where that is 0); a call clears what it uses of it, so
+ * that calls on one stream may share it.
  * No output may overlap an input, but for h0 and hT.  T <= 2^30. */
 enum { OURO_RECURRENCE_STRIDE = 64 };
 int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,

@@ -310,6 +310,7 @@ static const char* recurrence_refusal(int dtype, int B, int T, int D, int ldz, i
   if (B < 1 || T < 1 || T > ROWS_MAX || D < 1) return "bad sizes";
   if (ldz < D || ldx < D || ldo < D) return "a leading dimension below D";
   if (!scratch && recurrence_scratch_floats(B, T, D)) return "these sizes need scratch";
+  if (reinterpret_cast<uintptr_t>(scratch) & 15) return "scratch is not 16-byte aligned";
   return nullptr;
 }
 extern "C" int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,

@@ -19,23 +19,23 @@ template <typename T, int N> __device__ __forceinline__ void store_unaligned(T* 
   *reinterpret_cast<UnalignedPack<T, N>*>(p) = u;
 }
 
-// Which columns of a row of D a lane owns: strips of up to 8 lanes, P columns a lane.  The last lane of a row that is no
+// Which columns of a row of D a lane owns: strips of up to LANES lanes, P columns a lane.  The last lane of a row that is no
 // whole number of P moves back to the last P columns and shares some with the lane before it, which computes the same values; the two
 // are always lanes of one strip (a last strip of a single lane takes its neighbour over), so that what is read, changed and written
 // belongs to one workgroup.  Rows of fewer than P columns have one lane and go element by element (WHOLE false).
-constexpr int STRIP_LANES = 8;
+constexpr int STRIP_LANES = 8;                              // of 16 bytes a lane: 128 bytes
 struct LaneColumns {
   int col;
   int n;                                                   // 0, or the columns owned: P (WHOLE) or D
 };
-template <int P> __host__ __device__ __forceinline__ int strip_count(int D) {
-  return ((D + P - 1) / P + STRIP_LANES - 1) / STRIP_LANES;
+template <int P, int LANES = STRIP_LANES> __host__ __device__ __forceinline__ int strip_count(int D) {
+  return ((D + P - 1) / P + LANES - 1) / LANES;
 }
-template <int P, bool WHOLE> __device__ __forceinline__ LaneColumns lane_columns(int strip, int lane, int D) {
+template <int P, bool WHOLE, int LANES = STRIP_LANES> __device__ __forceinline__ LaneColumns lane_columns(int strip, int lane, int D) {
   if (!WHOLE) return {0, lane == 0 ? D : 0};
-  const int lanes = (D + P - 1) / P, strips = strip_count<P>(D);
-  int l = strip * STRIP_LANES + lane;
-  if (lanes > 1 && lanes % STRIP_LANES == 1) {
+  const int lanes = (D + P - 1) / P, strips = strip_count<P, LANES>(D);
+  int l = strip * LANES + lane;
+  if (lanes > 1 && lanes % LANES == 1) {
     if (strip == strips - 1) l = lane < 2 ? lanes - 2 + lane : lanes;
     else if (l == lanes - 2) l = lanes;
   }

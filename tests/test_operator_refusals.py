@@ -28,7 +28,8 @@ def test_embed_bwd_sorted(change):
 FWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, h0=None, lens=None, h=X, ldh=8, hT=None, states=None, scratch=None)
 BWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, states=X, lens=None, dh=X, lddh=8, dhT=None, dz=X, lddz=8, dx=X, lddx=8, dh0=None,
            scratch=None)
-SIZES = [dict(dtype=2), dict(B=0), dict(T=0), dict(D=0), dict(T=(1 << 30) + 1), dict(z=None), dict(x=None), dict(ldz=7), dict(ldx=7), dict(T=100000)]
+SIZES = [dict(dtype=2), dict(B=0), dict(T=0), dict(D=0), dict(T=(1 << 30) + 1), dict(z=None), dict(x=None), dict(ldz=7), dict(ldx=7), dict(T=100000),
+         dict(T=100000, scratch=C.c_void_p(4104))]
 
 
 @pytest.mark.parametrize("change", SIZES + [dict(h=None), dict(ldh=7)])
