@@ -10,8 +10,8 @@
 // Bound by memory: z, x (and dh) read once, h (or dz, dx) written once.  A workgroup owns 128 bytes of channels of one stream and a
 // tile of steps (256 in bf16, 512 in fp32, backward half of that).  Where streams and channels fill the chip it walks over its tiles itself.  Where they do not,
 // every tile has a workgroup: it publishes its map, reads those of up to RC_BACK tiles before it and the state behind the tile
-// before these, and publishes the state behind itself.  Tiles are dealt by a counter, so that a workgroup only waits for
-// workgroups that have begun before it and every wait ends.  Nothing is read twice.
+// before these, and publishes the state behind itself.  The tiles of a line (a strip of a stream) are dealt by a counter, so that a
+// workgroup only waits for workgroups that have begun before it and every wait ends.  Nothing is read twice.
 #include "common.h"
 #include "unaligned.h"
 
@@ -21,7 +21,7 @@ namespace ouro {
 
 constexpr int RC_WAVES = 8;                                // most waves of a workgroup
 constexpr int RC_BACK = 8;                                 // tiles whose maps a workgroup looks back over
-constexpr int RC_TICKET_BYTES = 64;
+constexpr int RC_TICKET_BYTES = 64;                        // of a line: the tickets of one counter for all, 13 ns each, would delay the last of 512 workgroups by 6 us
 constexpr int RC_P = 4;                                    // channels of a lane
 constexpr int RC_FWD = 8, RC_BWD = 4;                      // and consecutive steps: as many as let two workgroups share a CU (128 registers)
 template <typename T, int STEPS_OF_LANE = RC_FWD> struct RcShape {
@@ -41,7 +41,7 @@ struct RecurrenceParams {
   void* h; void* dz; void* dx;
   size_t ldh, lddz, lddx;
   float* hT; float* dh0; float* states;
-  unsigned* ticket;
+  unsigned* tickets;                                       // of every line, RC_TICKET_BYTES apart
   unsigned long long* maps;                                // [tile][B][D]: the map of a tile, factor below, offset above; 0: not there yet
   unsigned* behind;                                        // [tile][B][D]: the state behind a tile; 0: not there yet
 };
@@ -60,11 +60,23 @@ __device__ __forceinline__ void rc_gate(float z, float& f, float& e) {
   e = z >= 0.f ? q : r;
 }
 
+// Both in one register: the smaller of them with the sign of z; 1 - it is the other one to half a step.
+__device__ __forceinline__ float rc_pack(float z) {
+  const float t = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(z));
+  return copysignf(t * __builtin_amdgcn_rcpf(1.f + t), z);
+}
+__device__ __forceinline__ void rc_unpack(float& s, float& f, float& e) {
+  asm("" : "+v"(s));                                       // the compiler would hold both numbers of every step from the first time on
+  const float small = fabsf(s), large = 1.f - small;
+  const bool keep = __float_as_uint(s) >> 31 == 0;
+  f = keep ? large : small;
+  e = keep ? small : large;
+}
+
 // What a thread needs to find its elements.
 struct RcPlace {
   int b, col, ncol, wave, row, lane, waves, len;
   size_t base;                                             // row of step 0
-  size_t state;                                            // element of the first channel in [B][D]
 };
 template <typename T, bool WHOLE>
 __device__ __forceinline__ RcPlace rc_place(const RecurrenceParams& p, int strip, int b) {
@@ -79,7 +91,6 @@ __device__ __forceinline__ RcPlace rc_place(const RecurrenceParams& p, int strip
   a.ncol = own.n;
   a.len = p.lens ? max(0, min(p.T, p.lens[b])) : p.T;
   a.base = (size_t)b * p.T;
-  a.state = (size_t)b * p.D + a.col;
   return a;
 }
 
@@ -145,109 +156,93 @@ __device__ __forceinline__ void rc_wave_scan(const RcPlace& a, float (&A)[RC_P],
   }
 }
 
-// The state that enters tile `nth` in the order of the scan, in every thread, given the tile's own map (A, H).  `from`: h0 or dhT.
-// The first tile publishes a map that holds the state before it (factor 0), which later tiles therefore do not read.  The rows of
-// the first wave look back over RC_BACK / ROWS tiles each and compose what they find like steps.
+// Between the waves of a workgroup the first wave goes on with a channel a lane: the column of lane k is that of channel k % 4 of
+// lane k / 4 of the strip.
+struct RcChannel {
+  bool on;
+  size_t state;                                            // element in [B][D]
+};
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void rc_enter(const RecurrenceParams& p, const RcPlace& a, int nth, const float* from, const float (&A)[RC_P], const float (&H)[RC_P],
-                                         float (&state)[RC_P], float* shared) {
-  constexpr int ROWS = RcShape<T>::ROWS, LANES = RcShape<T>::LANES, PER = RC_BACK / ROWS;
+__device__ __forceinline__ RcChannel rc_channel(const RecurrenceParams& p, int strip, int b) {
+  const int k = threadIdx.x & 63;
+  const LaneColumns own = lane_columns<RC_P, WHOLE, RcShape<T>::LANES>(strip, min(k / RC_P, RcShape<T>::LANES - 1), p.D);
+  return {k < RcShape<T>::W && k % RC_P < own.n, (size_t)b * p.D + own.col + k % RC_P};
+}
+// The state that enters tile `nth` in the order of the scan, given the tile's own map (A, H).  `from`: h0 or dhT.
+// The first tile publishes a map that holds the state before it (factor 0), which later tiles therefore do not read.
+__device__ __forceinline__ float rc_enter(const RecurrenceParams& p, const RcChannel& c, int nth, const float* from, float A, float H) {
   const size_t stride = (size_t)p.B * p.D;                 // of tiles
-  if (a.wave == 0) {
-    float f[RC_P], h[RC_P];                                // the map from what precedes the row's tiles to what follows them
+  float state = 0.f;
+  if (nth == 0) {
+    if (c.on && from) state = from[c.state];
+    if (c.on && p.tiles > 1) rc_post(p.maps + c.state, (unsigned long long)rc_code(fmaf(A, state, H)) << 32 | rc_code(0.f));
+  } else {
+    if (c.on && nth + 1 < p.tiles) rc_post(p.maps + nth * stride + c.state, (unsigned long long)rc_code(H) << 32 | rc_code(A));
+    const int m0 = max(0, nth - RC_BACK);                  // the first tile looked at; the state behind the one before it is there, too
+    unsigned long long m[RC_BACK];
+    unsigned before = 1;
+    bool wait = true;
+    while (wait) {                                         // what is there stays there
+      wait = false;
+      if (c.on && m0 > 0) wait = (before = rc_peek(p.behind + (m0 - 1) * stride + c.state)) == 0;
 #pragma unroll
-    for (int j = 0; j < RC_P; ++j) { f[j] = 1.f; h[j] = 0.f; }
-    if (nth == 0 && from) load_columns<float, RC_P, WHOLE>(from + a.state, h, a.ncol);
-    if (a.row == 0 && nth + 1 < p.tiles)
-#pragma unroll
-      for (int j = 0; j < RC_P; ++j)
-        if (j < a.ncol)
-          rc_post(p.maps + nth * stride + a.state + j,
-                  (unsigned long long)rc_code(nth == 0 ? fmaf(A[j], h[j], H[j]) : H[j]) << 32 | rc_code(nth == 0 ? 0.f : A[j]));
-    if (nth > 0) {
-      const int m0 = max(0, nth - RC_BACK);                // the first tile looked at; the state behind the one before it is there, too
-      const int mine = m0 + a.row * PER;
-      unsigned long long m[PER][RC_P];
-      unsigned c[RC_P];
-      bool wait = true;
-      while (wait) {                                       // what is there stays there
-        wait = false;
-#pragma unroll
-        for (int j = 0; j < RC_P; ++j) {
-          c[j] = 1;
-          if (j < a.ncol && a.row == 0 && m0 > 0) c[j] = rc_peek(p.behind + (m0 - 1) * stride + a.state + j);
-          wait |= c[j] == 0;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            m[i][j] = 1;
-            if (j < a.ncol && mine + i < nth) m[i][j] = rc_peek(p.maps + (mine + i) * stride + a.state + j);
-            wait |= m[i][j] == 0;
-          }
-        }
-        wait = __any(wait);
-        if (wait) __builtin_amdgcn_s_sleep(1);
+      for (int i = 0; i < RC_BACK; ++i) {
+        m[i] = 1;
+        if (c.on && m0 + i < nth) m[i] = rc_peek(p.maps + (m0 + i) * stride + c.state);
       }
 #pragma unroll
-      for (int j = 0; j < RC_P; ++j) {
-        if (a.row == 0 && m0 > 0) { f[j] = 0.f; h[j] = rc_value(c[j]); }
+      for (int i = 0; i < RC_BACK; ++i) wait |= m[i] == 0;
+      wait = __any(wait);
+      if (wait) __builtin_amdgcn_s_sleep(1);
+    }
+    if (m0 > 0) state = rc_value(before);
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (mine + i < nth) {
-            const float mf = rc_value((unsigned)m[i][j]), mh = rc_value((unsigned)(m[i][j] >> 32));
-            h[j] = mine + i == 0 ? mh : fmaf(mf, h[j], mh);
-            f[j] *= mf;
-          }
+    for (int i = 0; i < RC_BACK; ++i)
+      if (m0 + i < nth) {
+        const float f = rc_value((unsigned)m[i]), h = rc_value((unsigned)(m[i] >> 32));
+        state = m0 + i == 0 ? h : fmaf(f, state, h);
       }
-#pragma unroll
-      for (int o = 1; o < ROWS; o <<= 1)
-#pragma unroll
-        for (int j = 0; j < RC_P; ++j) {
-          const float pf = __shfl_up(f[j], o * LANES, 64), ph = __shfl_up(h[j], o * LANES, 64);
-          if (a.row >= o) { h[j] = fmaf(f[j], ph, h[j]); f[j] *= pf; }
-        }
-    }
-    if (a.row == (nth > 0 ? ROWS - 1 : 0)) {
-      if (nth + 1 < p.tiles && p.tiles > RC_BACK + 1)
-#pragma unroll
-        for (int j = 0; j < RC_P; ++j)
-          if (j < a.ncol) rc_post(p.behind + nth * stride + a.state + j, rc_code(fmaf(A[j], h[j], H[j])));
-#pragma unroll
-      for (int j = 0; j < RC_P; ++j) shared[a.lane * RC_P + j] = h[j];
-    }
   }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < RC_P; ++j) state[j] = shared[a.lane * RC_P + j];
+  if (c.on && nth + 1 < p.tiles && p.tiles > RC_BACK + 1) rc_post(p.behind + nth * stride + c.state, rc_code(fmaf(A, state, H)));
+  return state;
 }
 
-// The strip, stream and (chained) tile of a workgroup.
+// How a stream's tiles are dealt: there is one; a workgroup walks over them; each has a workgroup.
+enum { RC_SINGLE, RC_WALK, RC_CHAINED };
+// The strip, stream and first tile of a workgroup.
 struct RcWork { int strip, b, nth; };
-template <bool CHAINED>
+template <int MODE>
 __device__ __forceinline__ RcWork rc_work(const RecurrenceParams& p, unsigned* shared) {
-  unsigned w = blockIdx.x;
-  if (CHAINED) {
-    if (threadIdx.x == 0) *shared = atomicAdd(p.ticket, 1u);
+  // Workgroups go to the 8 XCDs in turn; an XCD takes neighbouring lines: where rows do not start on cache lines, neighbouring strips
+  // share them, and one L2 then fetches and writes them whole.
+  const unsigned lines = (unsigned)p.strips * p.B, r = blockIdx.x % lines, xcd = r & 7;
+  const unsigned line = xcd * (lines >> 3) + min(xcd, lines & 7) + (r >> 3);
+  int nth = 0;
+  if (MODE == RC_CHAINED) {
+    if (threadIdx.x == 0) *shared = atomicAdd(p.tickets + line * (RC_TICKET_BYTES / 4), 1u);
     __syncthreads();
-    w = (unsigned)__builtin_amdgcn_readfirstlane((int)*shared);
+    nth = __builtin_amdgcn_readfirstlane((int)*shared);
   }
-  const unsigned lines = (unsigned)p.strips * p.B, line = w % lines;
-  return {(int)(line % p.strips), (int)(line / p.strips), (int)(w / lines)};
+  return {(int)(line % p.strips), (int)(line / p.strips), nth};
 }
 
-// WHOLE: see lane_columns.  CHAINED: a workgroup a tile.
-template <typename T, bool WHOLE, bool CHAINED>
+// WHOLE: see lane_columns.
+template <typename T, bool WHOLE, int MODE>
 __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_fwd_kernel(RecurrenceParams p) {
   using S = RcShape<T>;
-  __shared__ float sA[2][RC_WAVES][S::W], sH[2][RC_WAVES][S::W], enter[S::W];
+  __shared__ __align__(16) float sA[RC_WAVES][S::W], sH[RC_WAVES][S::W], enter[RC_WAVES][S::W];
   __shared__ unsigned ticket;
-  const RcWork work = rc_work<CHAINED>(p, &ticket);
+  const RcWork work = rc_work<MODE>(p, &ticket);
   const RcPlace a = rc_place<T, WHOLE>(p, work.strip, work.b);
-  const int steps = a.waves * S::STEPS;
-  float state[RC_P] = {};                                  // what enters the tile
-  if (!CHAINED && p.h0) load_columns<float, RC_P, WHOLE>(p.h0 + a.state, state, a.ncol);
-  int buf = 0, nth = work.nth;
+  const RcChannel c = rc_channel<T, WHOLE>(p, work.strip, work.b);
+  const int k = min((int)(threadIdx.x & 63), S::W - 1);     // (lanes without a channel read along)
+  const bool channel = (int)(threadIdx.x & 63) < S::W;
+  const int waves = MODE == RC_SINGLE ? a.waves : RC_WAVES, steps = waves * S::STEPS;
+  float carry = 0.f;                                       // first wave, channel k: the state that enters the tile, then the next wave
+  if (MODE != RC_CHAINED && a.wave == 0 && c.on && p.h0) carry = p.h0[c.state];
+  int nth = work.nth;
   do {
-    const int tw = nth * steps + a.wave * S::STEPS, t = tw + a.row * S::L;
+    const int t = nth * steps + a.wave * S::STEPS + a.row * S::L;
     float f[S::L][RC_P], u[S::L][RC_P], A[RC_P], H[RC_P];
     {
       RcRaw<T> z[S::L], x[S::L];
@@ -266,85 +261,87 @@ __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_fwd_kernel(Recurr
           H[j] = fmaf(f[i][j], H[j], u[i][j]);
         }
     }
-    rc_wave_scan<S::ROWS, S::LANES, true>(a, A, H, &sA[buf][a.wave][a.lane * RC_P], &sH[buf][a.wave][a.lane * RC_P]);
+    rc_wave_scan<S::ROWS, S::LANES, true>(a, A, H, &sA[a.wave][a.lane * RC_P], &sH[a.wave][a.lane * RC_P]);
     __syncthreads();
-    float before_a[RC_P], before_h[RC_P], all_a[RC_P], all_h[RC_P];            // the maps of the waves before this one, and of the tile
+    if (a.wave == 0) {
+      // (what the waves left is read twice rather than held: every register here is one that all steps of the lane live beside)
+      if (MODE == RC_CHAINED) {
+        float all_a = 1.f, all_h = 0.f;
 #pragma unroll
-    for (int j = 0; j < RC_P; ++j) { all_a[j] = 1.f; all_h[j] = 0.f; }
-    for (int w = 0; w < a.waves; ++w)
-#pragma unroll
-      for (int j = 0; j < RC_P; ++j) {
-        if (w == a.wave) { before_a[j] = all_a[j]; before_h[j] = all_h[j]; }
-        const float m = sA[buf][w][a.lane * RC_P + j];
-        all_h[j] = fmaf(m, all_h[j], sH[buf][w][a.lane * RC_P + j]);
-        all_a[j] *= m;
+        for (int w = 0; w < RC_WAVES; ++w) { all_h = fmaf(sA[w][k], all_h, sH[w][k]); all_a *= sA[w][k]; }
+        carry = rc_enter(p, c, nth, p.h0, all_a, all_h);
       }
-    if (CHAINED) rc_enter<T, WHOLE>(p, a, nth, p.h0, all_a, all_h, state, enter);
+      asm volatile("" ::: "memory");
+#pragma unroll 4
+      for (int w = 0; w < waves; ++w) {
+        if (channel) enter[w][k] = carry;
+        carry = fmaf(sA[w][k], carry, sH[w][k]);
+      }
+    }
+    __syncthreads();
     float h[RC_P];
 #pragma unroll
-    for (int j = 0; j < RC_P; ++j) {
-      h[j] = fmaf(A[j], fmaf(before_a[j], state[j], before_h[j]), H[j]);
-      state[j] = fmaf(all_a[j], state[j], all_h[j]);
-    }
+    for (int j = 0; j < RC_P; ++j) h[j] = fmaf(A[j], enter[a.wave][a.lane * RC_P + j], H[j]);
     if (p.states && t % RC_KEEP == 0 && t < p.T)
       store_columns<float, RC_P, WHOLE>(p.states + ((size_t)a.b * ((p.T + RC_KEEP - 1) / RC_KEEP) + t / RC_KEEP) * p.D + a.col, h, a.ncol);
 #pragma unroll
     for (int i = 0; i < S::L; ++i) {
-#pragma unroll
-      for (int j = 0; j < RC_P; ++j) h[j] = fmaf(f[i][j], h[j], u[i][j]);
       float out[RC_P];
 #pragma unroll
-      for (int j = 0; j < RC_P; ++j) out[j] = t + i < a.len ? h[j] : 0.f;
+      for (int j = 0; j < RC_P; ++j) {
+        h[j] = fmaf(f[i][j], h[j], u[i][j]);
+        out[j] = t + i < a.len ? h[j] : 0.f;
+      }
       if (t + i < p.T) rc_store<T, WHOLE>(a, p.h, p.ldh, t + i, out);
     }
-    buf ^= 1;
-  } while (++nth < p.tiles && !CHAINED);
-  if (nth == p.tiles && a.wave == 0 && a.row == 0 && p.hT) store_columns<float, RC_P, WHOLE>(p.hT + a.state, state, a.ncol);
+  } while (++nth < p.tiles && MODE == RC_WALK);
+  if (nth == p.tiles && a.wave == 0 && c.on && p.hT) p.hT[c.state] = carry;
 }
 
 // Tiles from the last one on.
-template <typename T, bool WHOLE, bool CHAINED>
+template <typename T, bool WHOLE, int MODE>
 __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_bwd_kernel(RecurrenceParams p) {
   using S = RcShape<T, RC_BWD>;
-  __shared__ float sA[2][RC_WAVES][S::W], sH[2][RC_WAVES][S::W], sQ[2][RC_WAVES][S::W], enter[S::W];
+  constexpr int KEPT = RC_KEEP / S::STEPS;                 // waves that share a kept state
+  __shared__ __align__(16) float sA[RC_WAVES][S::W], sH[RC_WAVES][S::W], sQ[RC_WAVES][S::W], enter[RC_WAVES][S::W], state[RC_WAVES][S::W];
   __shared__ unsigned ticket;
-  const RcWork work = rc_work<CHAINED>(p, &ticket);
+  const RcWork work = rc_work<MODE>(p, &ticket);
   const RcPlace a = rc_place<T, WHOLE>(p, work.strip, work.b);
-  const int steps = a.waves * S::STEPS;
-  float state[RC_P] = {};                                  // P of the step behind the tile
-  if (!CHAINED && p.dhT) load_columns<float, RC_P, WHOLE>(p.dhT + a.state, state, a.ncol);
-  int buf = 0, nth = work.nth;
+  const RcChannel c = rc_channel<T, WHOLE>(p, work.strip, work.b);
+  const int k = min((int)(threadIdx.x & 63), S::W - 1);     // (lanes without a channel read along)
+  const bool channel = (int)(threadIdx.x & 63) < S::W;
+  const int waves = MODE == RC_SINGLE ? a.waves : RC_WAVES, steps = waves * S::STEPS;
+  float carry = 0.f;                                       // first wave, channel k: P of the step behind the tile, then behind the wave before
+  if (MODE != RC_CHAINED && a.wave == 0 && c.on && p.dhT) carry = p.dhT[c.state];
+  int nth = work.nth;
   do {
-    const int tw = (p.tiles - 1 - nth) * steps + a.wave * S::STEPS, t = tw + a.row * S::L;
+    const int tile = (p.tiles - 1 - nth) * steps, t = tile + a.wave * S::STEPS + a.row * S::L;
     RcRaw<T> g[S::L];
-    // The smaller of f and 1 - f with the sign of z (both follow from it: 1 - it is exact to half a step of a number above a half);
-    // x, then h_{t-1} - x_t.
-    float s[S::L][RC_P], v[S::L][RC_P], kept[RC_P] = {};
-    float A[RC_P], H[RC_P], B[RC_P], Q[RC_P];
-    auto gates = [&](float& q, float& f, float& e) __attribute__((always_inline)) {
-      asm("" : "+v"(q));                                   // the compiler would keep both numbers of every step from the first time on
-      const float small = fabsf(q), large = 1.f - small;
-      const bool keep = __float_as_uint(q) >> 31 == 0;
-      f = keep ? large : small;
-      e = keep ? small : large;
-    };
+    float s[S::L][RC_P], v[S::L][RC_P];                    // see rc_pack; x, then h_{t-1} - x_t
+    float A[RC_P], H[RC_P], B[RC_P], Q[RC_P], kept[RC_WAVES / KEPT];
+    const int keeper = waves > 1 ? 1 : 0;                  // the wave that brings in the kept states
     {
       RcRaw<T> z[S::L], x[S::L];
       rc_load<T, WHOLE>(p, a, p.z, p.ldz, t, INFINITY, z);
-      rc_load<T, WHOLE>(p, a, p.x, p.ldx, t, 0.f, x);
       rc_load<T, WHOLE>(p, a, p.dh, p.lddh, t, 0.f, g);
-      if (tw < p.T) load_columns<float, RC_P, WHOLE>(p.states + ((size_t)a.b * ((p.T + RC_KEEP - 1) / RC_KEEP) + tw / RC_KEEP) * p.D + a.col, kept, a.ncol);
+      rc_load<T, WHOLE>(p, a, p.x, p.ldx, t, 0.f, x);
+      if (a.wave == keeper) {
+#pragma unroll
+        for (int i = 0; i < RC_WAVES / KEPT; ++i) {
+          kept[i] = 0.f;
+          if (c.on && tile + i * RC_KEEP < p.T) kept[i] = p.states[((size_t)a.b * ((p.T + RC_KEEP - 1) / RC_KEEP - 1) + tile / RC_KEEP + i) * p.D + c.state];
+        }
+      }
 #pragma unroll
       for (int j = 0; j < RC_P; ++j) { A[j] = 1.f; H[j] = Q[j] = 0.f; }
 #pragma unroll
       for (int i = 0; i < S::L; ++i)
 #pragma unroll
         for (int j = 0; j < RC_P; ++j) {
-          const float zz = to_f32(z[i].v[j]), r = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(zz));
-          s[i][j] = copysignf(r * __builtin_amdgcn_rcpf(1.f + r), zz);
+          s[i][j] = rc_pack(to_f32(z[i].v[j]));
           v[i][j] = to_f32(x[i].v[j]);
           float f, e;
-          gates(s[i][j], f, e);
+          rc_unpack(s[i][j], f, e);
           A[j] *= f;
           H[j] = fmaf(f, H[j], e * v[i][j]);
         }
@@ -354,45 +351,51 @@ __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_bwd_kernel(Recurr
 #pragma unroll
       for (int j = 0; j < RC_P; ++j) {
         float f, e;
-        gates(s[i][j], f, e);
+        rc_unpack(s[i][j], f, e);
         Q[j] = f * (to_f32(g[i].v[j]) + Q[j]);
       }
 #pragma unroll
     for (int j = 0; j < RC_P; ++j) B[j] = A[j];
-    rc_wave_scan<S::ROWS, S::LANES, false>(a, B, Q, &sA[buf][a.wave][a.lane * RC_P], &sQ[buf][a.wave][a.lane * RC_P]);
-    rc_wave_scan<S::ROWS, S::LANES, true>(a, A, H, nullptr, &sH[buf][a.wave][a.lane * RC_P]);
+    rc_wave_scan<S::ROWS, S::LANES, false>(a, B, Q, &sA[a.wave][a.lane * RC_P], &sQ[a.wave][a.lane * RC_P]);
+    rc_wave_scan<S::ROWS, S::LANES, true>(a, A, H, nullptr, &sH[a.wave][a.lane * RC_P]);
     __syncthreads();
-    float before_a[RC_P], before_q[RC_P], all_a[RC_P], all_q[RC_P];            // the maps of the waves behind this one, and of the tile
+    if (a.wave == keeper) {                                // the state that enters a wave: kept, or behind the wave before it
+      float h = 0.f;
 #pragma unroll
-    for (int j = 0; j < RC_P; ++j) { all_a[j] = 1.f; all_q[j] = 0.f; }
-    for (int w = a.waves - 1; w >= 0; --w)
-#pragma unroll
-      for (int j = 0; j < RC_P; ++j) {
-        if (w == a.wave) { before_a[j] = all_a[j]; before_q[j] = all_q[j]; }
-        const float m = sA[buf][w][a.lane * RC_P + j];
-        all_q[j] = fmaf(m, all_q[j], sQ[buf][w][a.lane * RC_P + j]);
-        all_a[j] *= m;
+      for (int w = 0; w < RC_WAVES; ++w) {
+        h = w % KEPT == 0 ? kept[w / KEPT] : MODE != RC_SINGLE || w < waves ? fmaf(sA[w - 1][k], h, sH[w - 1][k]) : 0.f;
+        if (channel) state[w][k] = h;
       }
-    // the state that enters the wave: kept, or one or more waves behind a kept one
-    for (int w = a.wave - (tw % RC_KEEP) / S::STEPS; w < a.wave; ++w)
+    }
+    if (a.wave == 0) {
+      if (MODE == RC_CHAINED) {
+        float all_a = 1.f, all_q = 0.f;
 #pragma unroll
-      for (int j = 0; j < RC_P; ++j) kept[j] = fmaf(sA[buf][w][a.lane * RC_P + j], kept[j], sH[buf][w][a.lane * RC_P + j]);
-    if (CHAINED) rc_enter<T, WHOLE>(p, a, nth, p.dhT, all_a, all_q, state, enter);
+        for (int w = RC_WAVES - 1; w >= 0; --w) { all_q = fmaf(sA[w][k], all_q, sQ[w][k]); all_a *= sA[w][k]; }
+        carry = rc_enter(p, c, nth, p.dhT, all_a, all_q);
+      }
+      asm volatile("" ::: "memory");
+#pragma unroll 4
+      for (int w = waves - 1; w >= 0; --w) {
+        if (channel) enter[w][k] = carry;
+        carry = fmaf(sA[w][k], carry, sQ[w][k]);
+      }
+    }
+    __syncthreads();
     float h[RC_P], q[RC_P];
 #pragma unroll
     for (int j = 0; j < RC_P; ++j) {
-      h[j] = fmaf(A[j], kept[j], H[j]);
-      q[j] = fmaf(B[j], fmaf(before_a[j], state[j], before_q[j]), Q[j]);
-      state[j] = fmaf(all_a[j], state[j], all_q[j]);
+      h[j] = fmaf(A[j], state[a.wave][a.lane * RC_P + j], H[j]);
+      q[j] = fmaf(B[j], enter[a.wave][a.lane * RC_P + j], Q[j]);
     }
 #pragma unroll
     for (int i = 0; i < S::L; ++i)
 #pragma unroll
       for (int j = 0; j < RC_P; ++j) {
-        float f, e;
-        gates(s[i][j], f, e);
         const float x = v[i][j];
         v[i][j] = h[j] - x;
+        float f, e;
+        rc_unpack(s[i][j], f, e);
         h[j] = fmaf(f, h[j], e * x);
       }
 #pragma unroll
@@ -400,9 +403,9 @@ __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_bwd_kernel(Recurr
       float dx[RC_P], dz[RC_P];
 #pragma unroll
       for (int j = 0; j < RC_P; ++j) {
-        float f, e;
-        gates(s[i][j], f, e);
         const float G = to_f32(g[i].v[j]) + q[j];
+        float f, e;
+        rc_unpack(s[i][j], f, e);
         dx[j] = e * G;
         dz[j] = G * v[i][j] * (f * e);
         q[j] = f * G;
@@ -413,13 +416,12 @@ __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_bwd_kernel(Recurr
         rc_store<T, WHOLE>(a, p.dz, p.lddz, t + i, dz);
       }
     }
-    buf ^= 1;
-  } while (++nth < p.tiles && !CHAINED);
-  if (nth == p.tiles && a.wave == 0 && a.row == 0 && p.dh0) store_columns<float, RC_P, WHOLE>(p.dh0 + a.state, state, a.ncol);
+  } while (++nth < p.tiles && MODE == RC_WALK);
+  if (nth == p.tiles && a.wave == 0 && c.on && p.dh0) p.dh0[c.state] = carry;
 }
 
 // How a call is laid out: a workgroup a tile where strips and streams alone are fewer workgroups than the chip holds (two a CU).
-struct RcPlan { int strips, waves, tiles, chained; };
+struct RcPlan { int strips, waves, tiles, mode; };
 static RcPlan rc_plan(int dtype, bool backward, int B, int T, int D) {
   RcPlan r;
   const int steps = (dtype == 1 ? RcShape<bf16_t>::ROWS : RcShape<float>::ROWS) * (backward ? RC_BWD : RC_FWD);
@@ -427,37 +429,37 @@ static RcPlan rc_plan(int dtype, bool backward, int B, int T, int D) {
   r.waves = 1;
   while (r.waves < RC_WAVES && (long long)r.waves * steps < T) r.waves *= 2;
   r.tiles = (int)(((long long)T + r.waves * steps - 1) / (r.waves * steps));
-  r.chained = r.tiles > 1 && (long long)B * r.strips < 512;
+  r.mode = r.tiles == 1 ? RC_SINGLE : (long long)B * r.strips < 512 ? RC_CHAINED : RC_WALK;
   return r;
 }
+static size_t rc_ticket_bytes(const RcPlan& r, int B) { return (size_t)r.strips * B * RC_TICKET_BYTES; }
 static size_t rc_map_count(const RcPlan& r, int B, int D) { return (size_t)r.tiles * B * D; }
-static size_t rc_scratch_bytes(const RcPlan& r, int B, int D) { return r.chained ? RC_TICKET_BYTES + (rc_map_count(r, B, D) * 12 + 15) / 16 * 16 : 0; }
+static size_t rc_scratch_bytes(const RcPlan& r, int B, int D) {
+  return r.mode == RC_CHAINED ? rc_ticket_bytes(r, B) + (rc_map_count(r, B, D) * 12 + 15) / 16 * 16 : 0;
+}
 size_t recurrence_scratch_floats(int B, int T, int D) {
   size_t n = 0;
   for (int i = 0; i < 4; ++i) n = std::max(n, rc_scratch_bytes(rc_plan(i & 1, i > 1, B, T, D), B, D));
   return n / 4;
 }
 
-template <typename T, bool WHOLE, bool CHAINED>
+template <typename T, bool WHOLE, int MODE>
 static void rc_launch(hipStream_t s, unsigned blocks, int waves, const RecurrenceParams& p, bool backward) {
-  if (backward) hipLaunchKernelGGL((recurrence_bwd_kernel<T, WHOLE, CHAINED>), dim3(blocks), dim3(64 * waves), 0, s, p);
-  else hipLaunchKernelGGL((recurrence_fwd_kernel<T, WHOLE, CHAINED>), dim3(blocks), dim3(64 * waves), 0, s, p);
+  if (backward) hipLaunchKernelGGL((recurrence_bwd_kernel<T, WHOLE, MODE>), dim3(blocks), dim3(64 * waves), 0, s, p);
+  else hipLaunchKernelGGL((recurrence_fwd_kernel<T, WHOLE, MODE>), dim3(blocks), dim3(64 * waves), 0, s, p);
 }
-template <typename T>
+template <typename T, bool WHOLE>
 static void rc_launch(hipStream_t s, unsigned blocks, const RcPlan& plan, const RecurrenceParams& p, bool backward) {
-  if (p.D >= RC_P) {
-    if (plan.chained) rc_launch<T, true, true>(s, blocks, plan.waves, p, backward);
-    else rc_launch<T, true, false>(s, blocks, plan.waves, p, backward);
-  } else {
-    if (plan.chained) rc_launch<T, false, true>(s, blocks, plan.waves, p, backward);
-    else rc_launch<T, false, false>(s, blocks, plan.waves, p, backward);
-  }
+  if (plan.mode == RC_SINGLE) rc_launch<T, WHOLE, RC_SINGLE>(s, blocks, plan.waves, p, backward);
+  else if (plan.mode == RC_WALK) rc_launch<T, WHOLE, RC_WALK>(s, blocks, plan.waves, p, backward);
+  else rc_launch<T, WHOLE, RC_CHAINED>(s, blocks, plan.waves, p, backward);
 }
 hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r) {
   const bool backward = r.dz != nullptr;
   const RcPlan plan = rc_plan(dtype, backward, r.B, r.T, r.D);
-  const long long blocks = (long long)r.B * plan.strips * (plan.chained ? plan.tiles : 1);
-  if (blocks * 64 * plan.waves >> 32 || (plan.chained && !r.scratch)) return hipErrorInvalidValue;
+  const bool chained = plan.mode == RC_CHAINED;
+  const long long blocks = (long long)r.B * plan.strips * (chained ? plan.tiles : 1);
+  if (blocks * 64 * plan.waves >> 32 || (chained && !r.scratch)) return hipErrorInvalidValue;
   RecurrenceParams p;
   memset(&p, 0, sizeof p);
   p.B = r.B; p.T = r.T; p.D = r.D; p.strips = plan.strips; p.tiles = plan.tiles;
@@ -465,16 +467,16 @@ hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r) 
   p.h0 = r.h0; p.dhT = r.dhT; p.lens = r.lens;
   p.h = r.h; p.dz = r.dz; p.dx = r.dx; p.ldh = r.ldh; p.lddz = r.lddz; p.lddx = r.lddx;
   p.hT = r.hT; p.dh0 = r.dh0; p.states = r.states;
-  if (plan.chained) {
+  if (chained) {
     char* at = reinterpret_cast<char*>(r.scratch);
-    p.ticket = reinterpret_cast<unsigned*>(at);
-    p.maps = reinterpret_cast<unsigned long long*>(at + RC_TICKET_BYTES);
+    p.tickets = reinterpret_cast<unsigned*>(at);
+    p.maps = reinterpret_cast<unsigned long long*>(at + rc_ticket_bytes(plan, r.B));
     p.behind = reinterpret_cast<unsigned*>(p.maps + rc_map_count(plan, r.B, r.D));
     const hipError_t e = launch_fill_zero(s, at, rc_scratch_bytes(plan, r.B, r.D));
     if (e != hipSuccess) return e;
   }
-  if (dtype == 1) rc_launch<bf16_t>(s, (unsigned)blocks, plan, p, backward);
-  else rc_launch<float>(s, (unsigned)blocks, plan, p, backward);
+  if (dtype == 1) r.D >= RC_P ? rc_launch<bf16_t, true>(s, (unsigned)blocks, plan, p, backward) : rc_launch<bf16_t, false>(s, (unsigned)blocks, plan, p, backward);
+  else r.D >= RC_P ? rc_launch<float, true>(s, (unsigned)blocks, plan, p, backward) : rc_launch<float, false>(s, (unsigned)blocks, plan, p, backward);
   return hipGetLastError();
 }
 
