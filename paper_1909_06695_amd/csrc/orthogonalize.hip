@@ -29,6 +29,7 @@ namespace ouro {
 
 typedef _Float16 half_t;
 typedef f16x8 half8;
+typedef __attribute__((ext_vector_type(4))) _Float16 half4;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float NS_SCALE = 4096.f, NS_DOWN = 1.f / 4096.f;
@@ -111,6 +112,9 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsParams p) {
   if (threadIdx.x == 0) p.sums[(size_t)b * p.parts + blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// What U is multiplied by, in 64 bits as the sum of squares.
+__device__ __forceinline__ double ns_factor(const NsParams& p, double squares) { return NS_SCALE / (sqrt(squares) + p.eps); }
+
 // X and its transpose, split and padded, from 64 x 64 tiles.
 template <typename T>
 __global__ __launch_bounds__(256) void ns_start_kernel(NsParams p) {
@@ -150,7 +154,7 @@ __global__ __launch_bounds__(256) void ns_start_kernel(NsParams p) {
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((tid & 63) == 0) part[tid >> 6] = sum;
   __syncthreads();
-  const double inv = NS_SCALE / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + p.eps);    // in 64 bits as the sum
+  const double inv = ns_factor(p, (part[0] + part[1]) + (part[2] + part[3]));
 #pragma unroll
   for (int k = 0; k < 16 / P; ++k) {
     const int at = tid + 256 * k, i = at / (64 / P), j = at % (64 / P) * P;
@@ -450,6 +454,243 @@ __global__ __launch_bounds__(512, 2) void ns_product_pp_kernel(NsParams p, NsPro
     ns_epilogue<KIND, T>(p, q, t.b, m_w + 128 * (i >> 2) + 32 * ((i >> 1) & 1), n_w + 128 * (i & 1), t.ti == t.tj, acc[i >> 1][i & 1], patch, lane);
 }
 
+// ------------------------------------------------------------- the small products of a pair
+// For m up to 64 what lies between A and C' C (or, of a single step, C) is one launch: a workgroup takes a matrix, four waves a 32 x 32 tile
+// of it each, and the two matrices that are needed at a time stay in LDS.  A launch per product costs its latency, 3 to 5 us (64 x 256:
+// 67 -> 49 us).  (At m = 128 the fragment reads take the LDS 2 us a product, and it gains nothing.)  Rows are as in memory, the 16-byte
+// chunks of row r at c ^ (r & 15).  All tiles are formed: what is stored for (n, m) is the value of (m, n).
+struct NsChain {
+  static constexpr int M = 64, ROW = M * 4, BYTES = M * ROW, TILES = M / 32, THREADS = 64 * TILES * TILES;
+  __device__ static __forceinline__ int at(int row, int chunk) { return row * ROW + ((chunk ^ (row & 15)) << 4); }
+  // acc = the tile of L R^T
+  __device__ static __forceinline__ void product(const char* l, const char* r, int ti, int tj, int lane, float (&v)[16]) {
+    f32x16 big, small;                                     // high x high, and the others
+#pragma unroll
+    for (int i = 0; i < 16; ++i) big[i] = small[i] = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < M / 32; ++kt) {
+      half8 a[4], b[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        a[c] = *reinterpret_cast<const half8*>(l + at(32 * ti + (lane & 31), kt * 8 + 2 * c + (lane >> 5)));
+        b[c] = *reinterpret_cast<const half8*>(r + at(32 * tj + (lane & 31), kt * 8 + 2 * c + (lane >> 5)));
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        big = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[c], b[c], big, 0, 0, 0);
+        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[c], b[2 + c], small, 0, 0, 0);
+        small = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[2 + c], b[c], small, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = (big[i] + small[i]) * NS_DOWN;
+  }
+  // v = a I + b A + c v
+  __device__ static __forceinline__ void polynomial(const char* a, int ti, int tj, int lane, float (&v)[16]) {
+    const int n = 32 * tj + (lane & 31);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int m = 32 * ti + 8 * r + 4 * (lane >> 5), chunk = ti * 8 + r, half = (lane >> 5) * 8;
+      const half4 hi = *reinterpret_cast<const half4*>(a + at(n, chunk) + half), lo = *reinterpret_cast<const half4*>(a + at(n, chunk + 4) + half);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        v[4 * r + e] = fmaf(NS_C, v[4 * r + e], fmaf(NS_B, (float)hi[e] + (float)lo[e], m + e == n ? NS_A * NS_SCALE : 0.f));
+    }
+  }
+  __device__ static __forceinline__ void store(char* to, int ti, int tj, int lane, const float (&v)[16]) {
+    const int n = 32 * tj + (lane & 31);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      half4 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        half_t h, l;
+        ns_split(v[4 * r + e], h, l);
+        hi[e] = h; lo[e] = l;
+      }
+      const int chunk = ti * 8 + r, half = (lane >> 5) * 8;
+      *reinterpret_cast<half4*>(to + at(n, chunk) + half) = hi;
+      *reinterpret_cast<half4*>(to + at(n, chunk + 4) + half) = lo;
+    }
+  }
+};
+// x: A, then C' C (two steps) or C, for the tile (ti, tj) of a wave that takes part; c: room for C.  All waves of the workgroup call.
+__device__ __forceinline__ void ns_chain(char* x, char* c, bool two, bool part, int ti, int tj, int lane) {
+  float v[16];
+  auto replace = [&](char* to, const char* l, const char* r, bool poly) __attribute__((always_inline)) {      // to <- l r^T, or (l = r = x) its polynomial
+    if (part) {
+      NsChain::product(l, r, ti, tj, lane, v);
+      if (poly) NsChain::polynomial(x, ti, tj, lane, v);
+    }
+    if (to == x) __syncthreads();
+    if (part) NsChain::store(to, ti, tj, lane, v);
+    __syncthreads();
+  };
+  replace(two ? c : x, x, x, true);
+  if (!two) return;
+#pragma unroll 1
+  for (int k = 0; k < 4; ++k) replace(x, k == 0 ? c : x, k == 0 || k == 2 ? x : c, k == 2);     // C A; C A C; C'; C' C
+}
+__global__ __launch_bounds__(NsChain::THREADS) void ns_chain_kernel(char* gram, int two) {
+  using K = NsChain;
+  extern __shared__ uint4 smem[];
+  char* x = reinterpret_cast<char*>(smem);
+  char* g = gram + (size_t)blockIdx.x * K::BYTES;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  for (int i = tid; i < K::BYTES / 16; i += K::THREADS)
+    *reinterpret_cast<uint4*>(x + K::at(i / (K::ROW / 16), i % (K::ROW / 16))) = reinterpret_cast<const uint4*>(g)[i];
+  __syncthreads();
+  ns_chain(x, x + K::BYTES, two, true, wave / K::TILES, wave % K::TILES, lane);
+  for (int i = tid; i < K::BYTES / 16; i += K::THREADS)
+    reinterpret_cast<uint4*>(g)[i] = *reinterpret_cast<const uint4*>(x + K::at(i / (K::ROW / 16), i % (K::ROW / 16)));
+}
+
+// ----------------------------------------------------------------------- a matrix a workgroup
+// Matrices up to 64 x 256 in one launch: a workgroup of 16 waves takes a matrix from the gradient to the result, X in LDS, a wave a 32 x 32
+// tile of it.  X X^T shares its contraction among four groups of waves; C' C times X reads X with the transposing LDS read and
+// replaces it in place.
+constexpr int NS_ALONE_COLS = 256, NS_ALONE_WAVES = 16;
+constexpr int NS_ALONE_PITCH = NS_ALONE_COLS * 4 + 16;     // bytes of a row of X: the next one 16 bytes further in the banks
+constexpr int NS_ALONE_X = 64 * NS_ALONE_PITCH, NS_ALONE_SUMS = 3 * 4 * 4096;
+constexpr int NS_ALONE_LDS = 2 * NsChain::BYTES + NS_ALONE_X + NS_ALONE_SUMS;
+template <typename T>
+__global__ __launch_bounds__(64 * NS_ALONE_WAVES) void ns_alone_kernel(NsParams p, int steps) {
+  extern __shared__ uint4 smem[];
+  char* const a = reinterpret_cast<char*>(smem);           // A ... C' C
+  char* const c = a + NsChain::BYTES;
+  char* const x = c + NsChain::BYTES;                      // [64][NS_ALONE_PITCH], rows as in memory
+  float4* const sums = reinterpret_cast<float4*>(x + NS_ALONE_X);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
+  // ---- U / (|U| + eps): 16 values a thread
+  constexpr int P = 16 / sizeof(T), CHUNKS = 16 / P;
+  const T* g = reinterpret_cast<const T*>(p.g) + b * p.sg;
+  float* mom = p.mom ? p.mom + b * p.sg : nullptr;
+  float u[CHUNKS][P];
+  double sum = 0;
+  const int per_row = (p.cols + P - 1) / P;                // pieces of the caller's rows: at most 64 x 256 / P + 256 of them
+#pragma unroll
+  for (int k = 0; k < CHUNKS; ++k) {
+    const int at = tid + 1024 * k, i = at / per_row, j = at % per_row * P;
+    const int n = i < p.rows ? min(P, p.cols - j) : 0;
+    const size_t o = i * p.ldg + j;
+    T v[P] = {};
+    if (n == P) load_unaligned<T, P>(g + o, v);
+    else
+#pragma unroll
+      for (int e = 0; e < P - 1; ++e)
+        if (e < n) v[e] = g[o + e];
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      float m = 0.f;
+      if (mom && e < n) mom[o + e] = m = fmaf(p.mu, mom[o + e], to_f32(v[e]));
+      u[k][e] = ns_update(p, to_f32(v[e]), m);
+      sum += (double)u[k][e] * u[k][e];
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) reinterpret_cast<double*>(sums)[wave] = sum;
+  for (int i = tid; i < NS_ALONE_X / 16; i += 1024) reinterpret_cast<uint4*>(x)[i] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+  sum = 0;
+  for (int w = 0; w < NS_ALONE_WAVES; ++w) sum += reinterpret_cast<double*>(sums)[w];
+  const double inv = ns_factor(p, sum);
+  auto put = [&](int m, int n, float v) __attribute__((always_inline)) {
+    half_t hi, lo;
+    ns_split(v, hi, lo);
+    char* at = x + m * NS_ALONE_PITCH + (n >> 5) * 128 + (n & 31) * 2;
+    *reinterpret_cast<half_t*>(at) = hi;
+    *reinterpret_cast<half_t*>(at + 64) = lo;
+  };
+#pragma unroll
+  for (int k = 0; k < CHUNKS; ++k) {
+    const int at = tid + 1024 * k, i = at / per_row, j = at % per_row * P;
+#pragma unroll
+    for (int e = 0; e < P; ++e)
+      if (i < p.rows && j + e < p.cols) put(p.tall ? j + e : i, p.tall ? i : j + e, (float)(u[k][e] * inv));
+  }
+  __syncthreads();
+  const int k_tiles = p.np / 32, tile = wave & 3, group = wave >> 2;
+  for (int i = 0; i < steps;) {
+    const bool two = i + 1 < steps;
+    // ---- A = X X^T
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    for (int kt = group; kt < k_tiles; kt += 4) {
+      half8 l[4], r[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        l[q] = *reinterpret_cast<const half8*>(x + (32 * (tile >> 1) + (lane & 31)) * NS_ALONE_PITCH + kt * 128 + q * 32 + (lane >> 5) * 16);
+        r[q] = *reinterpret_cast<const half8*>(x + (32 * (tile & 1) + (lane & 31)) * NS_ALONE_PITCH + kt * 128 + q * 32 + (lane >> 5) * 16);
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[q], r[q], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[q], r[2 + q], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(l[2 + q], r[q], acc, 0, 0, 0);
+      }
+    }
+    if (group > 0)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sums[(((group - 1) * 4 + tile) * 4 + r) * 64 + lane] = make_float4(acc[4 * r], acc[4 * r + 1], acc[4 * r + 2], acc[4 * r + 3]);
+    __syncthreads();
+    if (group == 0) {
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+          const float4 o = sums[((q * 4 + tile) * 4 + r) * 64 + lane];
+          acc[4 * r] += o.x; acc[4 * r + 1] += o.y; acc[4 * r + 2] += o.z; acc[4 * r + 3] += o.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * r + e] = acc[4 * r + e] * NS_DOWN;
+      }
+      NsChain::store(a, tile >> 1, tile & 1, lane, v);
+    }
+    __syncthreads();
+    ns_chain(a, c, two, wave < 4, tile >> 1, tile & 1, lane);
+    i += two ? 2 : 1;
+    // ---- X <- (C' C) X: the wave's tile, 32 rows ti of the polynomial and 32 columns tj of X
+    const int ti = wave & 1, tj = wave >> 1;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    if (tj < k_tiles) {
+      // the transposing read: 16 lanes fetch four rows of 16 columns and get four rows of a column each
+      const int g4 = lane >> 4, l16 = lane & 15;
+      const uint32_t from = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)x + (8 * (g4 >> 1) + (l16 >> 2)) * NS_ALONE_PITCH + tj * 128 + 2 * (16 * (g4 & 1) + 4 * (l16 & 3));
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        u32x2 r[4];
+        asm volatile(
+            "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %4 offset:%5\n\t"
+            "ds_read_b64_tr_b16 %2, %4 offset:64\n\tds_read_b64_tr_b16 %3, %4 offset:%6\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+            : "v"(from + ks * 16 * NS_ALONE_PITCH), "n"(4 * NS_ALONE_PITCH), "n"(4 * NS_ALONE_PITCH + 64)
+            : "memory");
+        const half8 rh = __builtin_bit_cast(half8, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3)), rl = __builtin_bit_cast(half8, __builtin_shufflevector(r[2], r[3], 0, 1, 2, 3));
+        const int chunk = (ks >> 1) * 8 + (ks & 1) * 2 + (lane >> 5);
+        const half8 lh = *reinterpret_cast<const half8*>(a + NsChain::at(32 * ti + (lane & 31), chunk)), ll = *reinterpret_cast<const half8*>(a + NsChain::at(32 * ti + (lane & 31), chunk + 4));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rh, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(lh, rl, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ll, rh, acc, 0, 0, 0);
+      }
+    }
+    __syncthreads();
+    if (tj < k_tiles) {
+      const int n = 32 * tj + (lane & 31);
+      T* o = reinterpret_cast<T*>(p.o) + b * p.so;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int m = 32 * ti + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+        if (i < steps) put(m, n, acc[r] * NS_DOWN);
+        else if (m < p.m && n < p.n) o[p.tall ? n * p.ldo + m : m * p.ldo + n] = from_f32<T>(acc[r] * (NS_DOWN * NS_DOWN) * p.scale);
+      }
+    }
+    __syncthreads();
+  }
+}
+
 // ---------------------------------------------------------------------------------- host
 static int ns_pad(int x) { return (x + 63) / 64 * 64; }
 static size_t ns_align(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -494,12 +735,19 @@ static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int 
 
 template <typename T>
 static hipError_t ns_run(hipStream_t s, NsParams& p, int batch, int steps) {
+  if (p.mp == 64 && p.np <= NS_ALONE_COLS) {
+    static bool allowed = false;
+    hipError_t e = pp_allow_lds((const void*)ns_alone_kernel<T>, NS_ALONE_LDS, allowed);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(ns_alone_kernel<T>, dim3(batch), dim3(64 * NS_ALONE_WAVES), NS_ALONE_LDS, s, p, steps);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(ns_norm_kernel<T>, dim3(p.parts, batch), dim3(256), 0, s, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(ns_start_kernel<T>, dim3(p.mp / 64 * (p.np / 64), batch), dim3(256), 0, s, p);
   e = hipGetLastError();
-  const bool pairs = p.np >= 2 * p.mp;                     // two steps with X once (see above); below, a pair is no less work
+  const bool pairs = p.np >= 2 * p.mp || p.mp == 64;       // two steps with X once (see above); below, a pair is no less work, but for small matrices fewer launches
   for (int i = 0, half = 0; i < steps && e == hipSuccess; half ^= 1) {
     const bool two = pairs && i + 1 < steps;
     auto product = [&](auto kind, const char* l, const char* r, int k_tiles, char* out) {
@@ -511,9 +759,15 @@ static hipError_t ns_run(hipStream_t s, NsParams& p, int batch, int steps) {
     constexpr std::integral_constant<int, NS_PLAIN> plain{};
     constexpr std::integral_constant<int, NS_POLY> poly{};
     product(plain, p.x, p.x, p.np / 32, p.gram);           // A
-    product(poly, p.gram, p.gram, p.mp / 32, p.c);         // C
-    const char* by = p.c;
-    if (two) {
+    const char* by = p.gram;
+    if (e == hipSuccess && p.mp == NsChain::M) {
+      hipLaunchKernelGGL(ns_chain_kernel, dim3(batch), dim3(NsChain::THREADS), 2 * NsChain::BYTES, s, p.gram, (int)two);
+      e = hipGetLastError();
+    } else {
+      product(poly, p.gram, p.gram, p.mp / 32, p.c);       // C
+      by = p.c;
+    }
+    if (two && p.mp != NsChain::M) {
       product(plain, p.c, p.gram, p.mp / 32, p.t);         // C A
       product(plain, p.t, p.c, p.mp / 32, p.gram);         // A' = C A C
       product(poly, p.gram, p.gram, p.mp / 32, p.t);       // C'
