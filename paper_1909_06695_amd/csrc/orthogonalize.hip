@@ -604,9 +604,24 @@ __global__ __launch_bounds__(64 * NS_ALONE_WAVES) void ns_alone_kernel(NsParams 
 #pragma unroll
   for (int k = 0; k < CHUNKS; ++k) {
     const int at = tid + 1024 * k, i = at / per_row, j = at % per_row * P;
+    if (i >= p.rows) continue;
+    if (p.tall) {
 #pragma unroll
-    for (int e = 0; e < P; ++e)
-      if (i < p.rows && j + e < p.cols) put(p.tall ? j + e : i, p.tall ? i : j + e, (float)(u[k][e] * inv));
+      for (int e = 0; e < P; ++e)
+        if (j + e < p.cols) put(j + e, i, (float)(u[k][e] * inv));
+    } else {                                               // (what lies past the columns is zero)
+      typedef _Float16 Piece __attribute__((ext_vector_type(P)));
+      Piece hi, lo;
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        half_t h, l;
+        ns_split((float)(u[k][e] * inv), h, l);
+        hi[e] = h; lo[e] = l;
+      }
+      char* to = x + i * NS_ALONE_PITCH + (j >> 5) * 128 + (j & 31) * 2;
+      *reinterpret_cast<Piece*>(to) = hi;
+      *reinterpret_cast<Piece*>(to + 64) = lo;
+    }
   }
   __syncthreads();
   const int k_tiles = p.np / 32, tile = wave & 3, group = wave >> 2;
