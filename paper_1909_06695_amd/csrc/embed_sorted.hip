@@ -404,8 +404,8 @@ hipError_t launch_embed_bwd_sorted(hipStream_t s, int dtype, const int32_t* tok,
   p.slices = dtype == 1 ? strip_count<8>(d) : strip_count<4>(d);
   // As many workgroups as the chip holds at once, two a CU, of which half clear rows where the matrix is overwritten; four
   // matrix rows each at least, and as many workgroups as keep the bit maps within their sizes.
-  p.clearers = accumulate ? 0 : std::min((vocab + 3) / 4, std::max(ES_CLEARERS, (int)((vocab + 32ll * ES_CAP - 1) / (32ll * ES_CAP))));
-  p.zero_rows = accumulate ? 0 : (vocab + p.clearers - 1) / p.clearers;
+  p.clearers = accumulate ? 0 : (int)std::min((vocab + 3ll) / 4, std::max((long long)ES_CLEARERS, (vocab + 32ll * ES_CAP - 1) / (32ll * ES_CAP)));
+  p.zero_rows = accumulate ? 0 : (int)((vocab - 1ll + p.clearers) / p.clearers);
   while (((long long)p.slices << (p.log2R + 1)) <= (accumulate ? 512 : 256) && (4ll << p.log2R) < vocab) ++p.log2R;
   while ((1ll << ES_ROW_BITS << p.log2R) < vocab) ++p.log2R;
   while ((1ll << p.row_bits << p.log2R) < vocab) ++p.row_bits;

@@ -143,3 +143,19 @@ def test_offsets_beyond_32_bits():
     ok(L().ouro_op_embed_bwd_sorted(stream(), 0, p(tok), p(dh), 8, p(out), ldv, 4, d, vocab, 1.0, 1))
     assert torch.equal(out[vocab - 1, :8], dh[0] + dh[2]) and torch.equal(out[vocab - 2, :8], dh[3]) and torch.equal(out[0, :8], dh[1])
     assert out.abs().sum() == dh.abs().sum()
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_the_largest_vocabulary(accumulate):
+    """2^31 - 1 rows of one column: the first, the last and one of a later workgroup's; everything else is cleared, or left as it was."""
+    vocab = 2**31 - 1
+    out = torch.ones(vocab, device="cuda")
+    tok = torch.tensor([vocab - 1, 0, vocab - 1, 1 << 30, -1], dtype=torch.int32, device="cuda")
+    dh = torch.tensor([[2.0], [3.0], [4.0], [5.0], [7.0]], device="cuda")
+    ok(L().ouro_op_embed_bwd_sorted(stream(), 0, p(tok), p(dh), 1, p(out), 1, 5, 1, vocab, 0.5, accumulate))
+    ref = {0: 1.5, 1 << 30: 2.5, vocab - 1: 3.0}
+    for at, value in ref.items():
+        assert out[at].item() == value + accumulate
+        out[at] = accumulate
+    step = 1 << 28
+    assert all((out[i:i + step] == accumulate).all() for i in range(0, vocab, step))
