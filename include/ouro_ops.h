@@ -177,7 +177,7 @@ int ouro_op_embed_bwd(void* stream, int dtype, const int32_t* tok, const void* d
 /* The same gradient with sums in an order that the ids alone determine: dV[v,:] = scale * sum of the rows dh[n,:] with
  * tok[n] = v, or with accumulate != 0 dV[v,:] += that (a tied matrix that already holds its other gradient: only the rows of
  * ids that occur are read and written).  dh [N, lddh] of type T, dV fp32 [vocab, ldv]; lddh, ldv >= d, any alignment of an
- * element.  Ids outside [0, vocab) take no part.  N = 0 is allowed (tok, dh are not used then); N <= 2^30.  One launch,
+ * element.  Ids outside [0, vocab) take no part.  N = 0 is allowed (tok, dh are not used then); N, d <= 2^30.  One launch,
  * no workspace; equal calls give equal bits. */
 int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv, int N,
                              int d, int vocab, float scale, int accumulate);
@@ -185,19 +185,19 @@ int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const 
  * z, x, h: rows b*T+t of type T (ld* in elements, >= D, any alignment of an element).  h0 fp32 [B, D], the state that enters
  * step 0 (NULL: zero); hT fp32 [B, D], the state behind the last step (may be NULL).  States are fp32 throughout.  z = +infinity
  * gives f = 1 (the state is kept), -infinity f = 0.  T = 1 is the form for single tokens; h0 and hT may then, as always, be one buffer.
- * lens: int32 [B], device, or NULL: stream b has lens[b] steps (taken as 0 below 0, as T above T); rows behind them are not
- * read, h is zero there, and the state stays what it is.
+ * lens: int32 [B], device, or NULL: stream b has lens[b] steps (taken as 0 below 0, as T above T); what the rows behind them
+ * hold does not matter, h is zero there, and the state stays what it is.
  * states: fp32 [B, ceil(T / OURO_RECURRENCE_STRIDE), D] or NULL: the state that enters every OURO_RECURRENCE_STRIDE-th
  * step, which is what the backward call needs.
  * scratch: fp32, ouro_op_recurrence_scratch() floats, 16-byte aligned (NULL where that is 0); a call clears what it uses of it, so
  * that calls on one stream may share it.
- * No output may overlap an input, but for h0 and hT.  T <= 2^30. */
+ * No output may overlap an input, but for h0 and hT.  T, D <= 2^30. */
 enum { OURO_RECURRENCE_STRIDE = 64 };
 int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
                            const float* h0, const int32_t* lens, void* h, int ldh, float* hT, float* states, float* scratch);
 /* Backward of the above from z, x, states and lens as they were: dh rows of type T, dhT fp32 [B, D] the gradient of hT (NULL:
  * zero).  dz, dx (type T) and dh0 (fp32 [B, D], may be NULL) are overwritten; rows behind a stream's length are zero in dz and dx,
- * and dh is not read there.  dhT and dh0 may be one buffer. */
+ * and what dh holds there does not matter.  dhT and dh0 may be one buffer. */
 int ouro_op_recurrence_bwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
                            const float* states, const int32_t* lens, const void* dh, int lddh, const float* dhT, void* dz,
                            int lddz, void* dx, int lddx, float* dh0, float* scratch);
@@ -229,10 +229,11 @@ int ouro_op_update_tiles(int rows, int cols, int ld_out);
  * momentum NULL: U = g.  Else momentum (fp32, laid out as g) becomes mu momentum + g, and U is the new momentum, with nesterov != 0
  * g + mu momentum.  g and o are of type T; matrix i begins sg (g, momentum) and so (o) elements behind matrix 0, rows ldg and ldo
  * apart, any alignment of an element.  Matrices of o, and of momentum, must not overlap: they lie one after the other or side by side in
- * wider rows (the parts of W_qkv).  o may be g.  A zero matrix stays zero (eps > 0); one with a NaN or infinity becomes NaN
+ * wider rows (the parts of W_qkv).  o may be g, laid out alike; nothing else may overlap.  A zero matrix stays zero (eps > 0); one with a NaN or infinity becomes NaN
  * whole, the others of the batch are not affected.  The arithmetic is nearly that of fp32 (22-bit operands, fp32
- * sums); entries of X below 2^-37 count as zero, which shows only where eps is many orders above |U|_F.  scratch: fp32, ouro_op_orthogonalize_scratch() floats, 16-byte aligned; 0 for sizes that are refused (padded to
- * multiples of 64, rows * cols < 2^29). */
+ * sums); entries of X below 2^-37 count as zero, which shows only where eps is many orders above |U|_F.
+ * scratch: fp32, ouro_op_orthogonalize_scratch() floats, 16-byte aligned; 0 for sizes that are refused (padded to multiples of 64,
+ * rows * cols < 2^29).  What it holds does not matter, so that calls on one stream may share it. */
 int ouro_op_orthogonalize(void* stream, int dtype, int batch, int rows, int cols, const void* g, int ldg, long long sg, float* momentum, float mu,
                           int nesterov, void* o, int ldo, long long so, float scale, float eps, int steps, float* scratch);
 size_t ouro_op_orthogonalize_scratch(int batch, int rows, int cols);

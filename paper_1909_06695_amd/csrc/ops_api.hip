@@ -295,7 +295,7 @@ extern "C" int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* 
                                         int d, int vocab, float scale, int accumulate) {
   const char* op = "embed_bwd_sorted";
   if (dtype < 0 || dtype > 1) return refuse(op, "dtype is 0 or 1");
-  if (N < 0 || N > ROWS_MAX || d < 1 || vocab < 1) return refuse(op, "bad sizes");
+  if (N < 0 || N > ROWS_MAX || d < 1 || d > ROWS_MAX || vocab < 1) return refuse(op, "bad sizes");
   if (!dV || (N && (!tok || !dh))) return refuse(op, "null pointer");
   if ((N && lddh < d) || ldv < d) return refuse(op, "a leading dimension below d");
   return rc_of(launch_embed_bwd_sorted((hipStream_t)stream, dtype, tok, dh, lddh, dV, ldv, N, d, vocab, scale, accumulate));
@@ -303,11 +303,11 @@ extern "C" int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* 
 
 static_assert(RECURRENCE_STRIDE == OURO_RECURRENCE_STRIDE, "the boundary names the distance of the kept states");
 extern "C" size_t ouro_op_recurrence_scratch(int B, int T, int D) {
-  return B < 1 || T < 1 || T > ROWS_MAX || D < 1 ? 0 : recurrence_scratch_floats(B, T, D);
+  return B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > ROWS_MAX ? 0 : recurrence_scratch_floats(B, T, D);
 }
 static const char* recurrence_refusal(int dtype, int B, int T, int D, int ldz, int ldx, int ldo, const float* scratch) {
   if (dtype < 0 || dtype > 1) return "dtype is 0 or 1";
-  if (B < 1 || T < 1 || T > ROWS_MAX || D < 1) return "bad sizes";
+  if (B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > ROWS_MAX) return "bad sizes";
   if (ldz < D || ldx < D || ldo < D) return "a leading dimension below D";
   if (!scratch && recurrence_scratch_floats(B, T, D)) return "these sizes need scratch";
   if (reinterpret_cast<uintptr_t>(scratch) & 15) return "scratch is not 16-byte aligned";
@@ -404,6 +404,7 @@ extern "C" int ouro_op_orthogonalize(void* stream, int dtype, int batch, int row
   if (ldg < cols || ldo < cols) return refuse(op, "a leading dimension below cols");
   if (sg < 0 || !matrices_apart(batch, rows, cols, ldo, so) || (momentum && !matrices_apart(batch, rows, cols, ldg, sg)))
     return refuse(op, "matrices that overlap");
+  if (o == g && (ldo != ldg || (batch > 1 && so != sg))) return refuse(op, "o is g in another layout");
   if (!(eps >= 0.f) || steps < 1 || steps > 100) return refuse(op, "eps is not negative, steps 1 to 100");
   if (reinterpret_cast<uintptr_t>(scratch) & 15) return refuse(op, "scratch is not 16-byte aligned");
   OrthogonalizeDesc d;
