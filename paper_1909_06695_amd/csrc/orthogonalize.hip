@@ -6,7 +6,7 @@
 // mantissa): x y = xh yh + xh yl + xl yh with fp32 accumulation.  One fp16 (or bf16) number is not enough: a step multiplies small singular
 // values by a, five steps by 485, and with them the rounding noise of X: with 16 strong directions over noise of 1e-4 one
 // fp16 number gives an error of 4.5e-2, bf16 0.37, the two halves 8e-6 and fp32 arithmetic 5e-6 (random matrices: 1.4e-3, 1.1e-2,
-// 2.6e-7, 1.7e-7).  All entries of X, A and the polynomial are below 5 in magnitude (|X|_2 <= 1.2); they are stored times 2^12, so that
+// 2.6e-7, 1.7e-7).  All entries of X, A and the polynomials are below 12 in magnitude (|X|_2 <= 1.2, |C|_2 <= 3.5); they are stored times 2^12, so that
 // the low halves of ordinary entries (1 / sqrt(rows cols)) stay above fp16's smallest normal number.
 //
 // With C = a I + b A + c A^2 a step is X <- C X, and the A of the step after it is C A C: all of these are polynomials of one symmetric
@@ -23,6 +23,7 @@
 #include "unaligned.h"
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace ouro {
@@ -34,6 +35,7 @@ typedef __attribute__((ext_vector_type(4))) _Float16 half4;
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float NS_SCALE = 4096.f, NS_DOWN = 1.f / 4096.f;
 constexpr int NS_NORM_PARTS = 256;                         // most partial sums of squares of a matrix
+constexpr int NS_ARRIVED = 4 * 128;                        // counters: of the waves of up to 128 tiles
 
 // A split matrix [rows][cols], cols a multiple of 32: a row holds per 32 columns the 32 high halves, then the 32 low ones.
 __device__ __forceinline__ size_t ns_at(int row, int col, int cols) {
@@ -54,6 +56,7 @@ struct NsParams {
   float scale, eps;
   int parts;
   double* sums;                                            // [batch][parts]
+  unsigned* arrived;                                       // [NS_ARRIVED]: see NsProduct; 0 between launches
   char *x, *xt[2], *gram, *c, *t;                          // split matrices, batch after batch
 };
 
@@ -67,6 +70,8 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsParams p) {
   constexpr int P = 16 / sizeof(T);
   __shared__ double part[4];
   const int b = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (blockIdx.x == 0 && b == 0)
+    for (int i = threadIdx.x; i < NS_ARRIVED; i += 256) p.arrived[i] = 0;
   const T* g = reinterpret_cast<const T*>(p.g) + b * p.sg;
   float* mom = p.mom ? p.mom + b * p.sg : nullptr;
   double sum = 0;
@@ -195,14 +200,20 @@ struct NsProduct {
   int tiles_b;                                             // tiles along rows_b; symmetric results: 0
   int tiles;                                               // of one matrix
   char* out; char* out_t;                                  // PLAIN, POLY: the result; NEXT: X and X^T
+  // PLAIN, few tiles and a long contraction: a tile has `splits` workgroups, each a range of `per` K-tiles.  They leave their sums in `parts`, wave
+  // by wave, and the wave that arrives last adds those of its piece up in order and goes on with the epilogue.
+  int splits, per;
+  double* parts;                                           // two sums each, [matrix][tile][split][wave][8][lane]
 };
 
 // The matrix and the tile of a workgroup.  Workgroups are dealt to the 8 XCDs in turn; an XCD takes a run of neighbouring tiles, whose
 // operands its L2 then shares.
-struct NsTile { int b, ti, tj; };
+struct NsTile { int b, ti, tj, split; };       // split: of q.splits > 1
 __device__ __forceinline__ NsTile ns_tile(const NsProduct& q) {
-  const int nb = gridDim.x, share = nb >> 3, rest = nb & 7, xcd = blockIdx.x & 7, bid = xcd * share + min(xcd, rest) + (blockIdx.x >> 3);
+  const int nb = gridDim.x, share = nb >> 3, rest = nb & 7, xcd = blockIdx.x & 7, at = xcd * share + min(xcd, rest) + (blockIdx.x >> 3);
+  const int bid = q.splits > 1 ? at / q.splits : at;
   NsTile r;
+  r.split = at - bid * q.splits;
   r.b = bid / q.tiles;
   const int t = bid - r.b * q.tiles;
   if (q.tiles_b) {
@@ -357,10 +368,12 @@ __global__ __launch_bounds__(256 * G) void ns_product_kernel(NsParams p, NsProdu
     oa[i] = (uint32_t)(m0 + row) * ld + off;
     ob[i] = (uint32_t)(n0 + row) * ld + off;
   }
-  const int mine = (q.k_tiles - group + G - 1) / G, most = (q.k_tiles + G - 1) / G;     // K-tiles group, group + G, ...
+  const bool split = KIND == NS_PLAIN && S == 1 && G == 4 && q.splits > 1;
+  const int k0 = split ? t.split * q.per : 0, k_tiles = split ? min(q.per, q.k_tiles - k0) : q.k_tiles;
+  const int mine = (k_tiles - group + G - 1) / G, most = (k_tiles + G - 1) / G;     // K-tiles group, group + G, ...
   auto request = [&](int i, int stage) __attribute__((always_inline)) {
     char* dst = lds + stage * STAGE + wave * 2 * S * 1024;
-    const uint32_t k = (uint32_t)(i * G + group) * 128;
+    const uint32_t k = (uint32_t)(k0 + i * G + group) * 128;
 #pragma unroll
     for (int r = 0; r < 2 * S; ++r) {
       ns_request(A, bytes_a, dst + r * 1024, oa[r], k);
@@ -424,6 +437,34 @@ __global__ __launch_bounds__(256 * G) void ns_product_kernel(NsParams p, NsProdu
           const float4 v = sums[(((g * 4 + wave) * S * S + i) * 4 + r) * 64 + lane];
           acc[i / S][i % S][4 * r] += v.x; acc[i / S][i % S][4 * r + 1] += v.y; acc[i / S][i % S][4 * r + 2] += v.z; acc[i / S][i % S][4 * r + 3] += v.w;
         }
+  }
+  if (split) {
+    // (Stores and loads that pass by the caches XCDs do not share, and the counter after the stores have arrived: fences, which write back and
+    // drop a whole L2, take 30 us here.)
+    const size_t tile = (size_t)t.b * q.tiles + t.ti * (t.ti + 1) / 2 + t.tj;
+    double* part = q.parts + ((tile * q.splits * 4 + wave) * 8) * 64 + lane;
+    constexpr int APART = 4 * 8 * 64;                      // of a split
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const float2 two = make_float2(acc[0][0][2 * r], acc[0][0][2 * r + 1]);
+      __hip_atomic_store(part + t.split * APART + r * 64, __builtin_bit_cast(double, two), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned* arrived = p.arrived + tile * 4 + wave;
+    unsigned nth = 0;
+    if (lane == 0) nth = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__builtin_amdgcn_readfirstlane((int)nth) + 1 < q.splits) return;
+    asm volatile("" ::: "memory");
+    if (lane == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][0][r] = 0.f;
+#pragma unroll 4
+    for (int k = 0; k < q.splits; ++k)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float2 two = __builtin_bit_cast(float2, __hip_atomic_load(part + k * APART + r * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        acc[0][0][2 * r] += two.x; acc[0][0][2 * r + 1] += two.y;
+      }
   }
   float* patch = reinterpret_cast<float*>(smem) + (G - 1) * 4 * S * S * 1024 + wave * NS_PATCH;      // behind the sums, which other waves may still read
 #pragma unroll
@@ -711,7 +752,7 @@ static int ns_pad(int x) { return (x + 63) / 64 * 64; }
 static size_t ns_align(size_t bytes) { return (bytes + 255) / 256 * 256; }
 size_t orthogonalize_scratch_floats(int batch, int rows, int cols) {
   const size_t mp = ns_pad(std::min(rows, cols)), np = ns_pad(std::max(rows, cols));
-  return (ns_align((size_t)batch * NS_NORM_PARTS * 8) + (size_t)batch * 4 * (3 * mp * np + 3 * mp * mp)) / 4;
+  return (ns_align((size_t)batch * NS_NORM_PARTS * 8) + NS_ARRIVED * 4 + (size_t)batch * 4 * (3 * mp * np + 3 * mp * mp)) / 4;
 }
 
 static long long ns_tiles(int edge, int rows_a, int rows_b, bool symmetric) {
@@ -726,17 +767,31 @@ static hipError_t ns_launch_small(hipStream_t s, dim3 grid, const NsParams& p, c
   hipLaunchKernelGGL((ns_product_kernel<S, G, KIND, T>), grid, dim3(256 * G), (NsSmall<S, G>::LDS), s, p, q);
   return hipGetLastError();
 }
-// One product of every matrix of the batch: 256 wide tiles where they fill the chip, else 128 wide ones, else 64; with 64 wide tiles
-// the contraction is dealt to four groups of waves where there is a workgroup a CU, else to two.  (One matrix of 1024 x 1024: four groups
-// 197 us, two 213, one 247; of 2048 x 2048: two 936, four 973, one 1060.)
+// One product of every matrix of the batch.  64 wide tiles where two workgroups a CU hold them all, with the contraction dealt to four groups
+// of waves where there is a workgroup a CU, else to two (one matrix of 1024 x 1024: four groups 197 us, two 213, one 247).  More of
+// them would take a second round: then 128 wide ones, in two groups where each CU has one (2048 x 2048: 64 wide 904 us, 128 wide in two groups
+// 791, in one 1071; six of 1024 x 1024: 64 wide 581, 531, 649), in one where each CU has more (24 of 768 x 2048: 1721, 1587, 1542);
+// and 256 wide ones where they fill the chip (24 of 1024 x 4096: 128 wide 4.4 ms, 3.7).  No tile is more than twice as wide as a matrix is high.
 template <int KIND, typename T>
 static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int batch) {
   const bool symmetric = KIND == NS_PLAIN || KIND == NS_POLY;
-  int edge = 256;
-  while (edge > 64 && ns_tiles(edge, q.rows_a, q.rows_b, symmetric) * batch < 192) edge /= 2;
+  auto tiles = [&](int edge) { return ns_tiles(edge, q.rows_a, q.rows_b, symmetric) * batch; };
+  const int edge = tiles(64) <= 512 || q.rows_a <= 64 ? 64 : tiles(256) < 192 || q.rows_a <= 128 ? 128 : 256;
   q.tiles = (int)ns_tiles(edge, q.rows_a, q.rows_b, symmetric);
   q.tiles_b = symmetric ? 0 : (q.rows_b + edge - 1) / edge;
-  const dim3 grid((unsigned)(q.tiles * batch));
+  // A workgroup a CU at most, whose share of the contraction costs it what the sums of the other shares cost the one that adds them up: n K-tiles at
+  // 0.09 us against k_tiles / n shares at 0.27 us.  (64 x 4096: 116 -> 68 us, 64 x 16384 362 -> 96, 410 x 2100 176 -> 153, 50257 x
+  // 128 1155 -> 255; 512 x 512 is as before.)  `parts` has the place of a matrix X.
+  if (q.parts && edge == 64) {
+    const long long room = (long long)p.mp * p.np / (q.tiles * 4096ll), share = std::max(8, (int)std::sqrt(3.0 * q.k_tiles));
+    const int want = (int)std::min({256ll / (q.tiles * batch), q.k_tiles / share, room});
+    if (want > 1) {
+      q.per = (q.k_tiles + want - 1) / want;
+      q.splits = (q.k_tiles + q.per - 1) / q.per;
+    }
+  }
+  const dim3 grid((unsigned)(q.tiles * batch * q.splits));
+  if (q.splits > 1) return ns_launch_small<1, 4, KIND, T>(s, grid, p, q);
   if (edge == 256) {
     static bool allowed = false;
     hipError_t e = pp_allow_lds((const void*)ns_product_pp_kernel<KIND, T>, PP_LDS, allowed);
@@ -744,7 +799,7 @@ static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int 
     hipLaunchKernelGGL((ns_product_pp_kernel<KIND, T>), grid, dim3(512), PP_LDS, s, p, q);
     return hipGetLastError();
   }
-  if (edge == 128) return ns_launch_small<2, 1, KIND, T>(s, grid, p, q);
+  if (edge == 128) return q.tiles * batch <= 256 ? ns_launch_small<2, 2, KIND, T>(s, grid, p, q) : ns_launch_small<2, 1, KIND, T>(s, grid, p, q);
   return q.tiles * batch <= 256 && q.k_tiles >= 8 ? ns_launch_small<1, 4, KIND, T>(s, grid, p, q) : ns_launch_small<1, 2, KIND, T>(s, grid, p, q);
 }
 
@@ -765,34 +820,37 @@ static hipError_t ns_run(hipStream_t s, NsParams& p, int batch, int steps) {
   const bool pairs = p.np >= 2 * p.mp || p.mp == 64;       // two steps with X once (see above); below, a pair is no less work, but for small matrices fewer launches
   for (int i = 0, half = 0; i < steps && e == hipSuccess; half ^= 1) {
     const bool two = pairs && i + 1 < steps;
-    auto product = [&](auto kind, const char* l, const char* r, int k_tiles, char* out) {
+    auto product = [&](auto kind, const char* l, const char* r, char* out) {
       NsProduct q;
       memset(&q, 0, sizeof q);
-      q.a = l; q.b = r; q.rows_a = q.rows_b = p.mp; q.k_tiles = k_tiles; q.out = out;
+      q.a = l; q.b = r; q.rows_a = q.rows_b = p.mp; q.k_tiles = (l == p.x ? p.np : p.mp) / 32; q.out = out;
+      q.splits = 1;
+      if (l == p.x) q.parts = reinterpret_cast<double*>(p.xt[1 - half]);    // free until X is written
       if (e == hipSuccess) e = ns_product<decltype(kind)::value, float>(s, p, q, batch);
     };
     constexpr std::integral_constant<int, NS_PLAIN> plain{};
     constexpr std::integral_constant<int, NS_POLY> poly{};
-    product(plain, p.x, p.x, p.np / 32, p.gram);           // A
+    product(plain, p.x, p.x, p.gram);                      // A
     const char* by = p.gram;
     if (e == hipSuccess && p.mp == NsChain::M) {
       hipLaunchKernelGGL(ns_chain_kernel, dim3(batch), dim3(NsChain::THREADS), 2 * NsChain::BYTES, s, p.gram, (int)two);
       e = hipGetLastError();
     } else {
-      product(poly, p.gram, p.gram, p.mp / 32, p.c);       // C
+      product(poly, p.gram, p.gram, p.c);                  // C
       by = p.c;
     }
     if (two && p.mp != NsChain::M) {
-      product(plain, p.c, p.gram, p.mp / 32, p.t);         // C A
-      product(plain, p.t, p.c, p.mp / 32, p.gram);         // A' = C A C
-      product(poly, p.gram, p.gram, p.mp / 32, p.t);       // C'
-      product(plain, p.t, p.c, p.mp / 32, p.gram);         // C' C
+      product(plain, p.c, p.gram, p.t);                    // C A
+      product(plain, p.t, p.c, p.gram);                    // A' = C A C
+      product(poly, p.gram, p.gram, p.t);                  // C'
+      product(plain, p.t, p.c, p.gram);                    // C' C
       by = p.gram;
     }
     i += two ? 2 : 1;
     if (e != hipSuccess) break;
     NsProduct q;
     memset(&q, 0, sizeof q);
+    q.splits = 1;
     q.a = by; q.b = p.xt[half]; q.rows_a = p.mp; q.rows_b = p.np; q.k_tiles = p.mp / 32; q.out = p.x; q.out_t = p.xt[1 - half];
     e = i < steps ? ns_product<NS_NEXT, float>(s, p, q, batch) : ns_product<NS_LAST, T>(s, p, q, batch);
   }
@@ -810,6 +868,7 @@ hipError_t launch_orthogonalize(hipStream_t s, int dtype, const OrthogonalizeDes
   const size_t big = (size_t)d.batch * p.mp * p.np * 4, small = (size_t)d.batch * p.mp * p.mp * 4;
   char* at = reinterpret_cast<char*>(d.scratch);
   p.sums = reinterpret_cast<double*>(at); at += ns_align((size_t)d.batch * NS_NORM_PARTS * 8);
+  p.arrived = reinterpret_cast<unsigned*>(at); at += NS_ARRIVED * 4;
   p.x = at; at += big;
   p.xt[0] = at; at += big;
   p.xt[1] = at; at += big;

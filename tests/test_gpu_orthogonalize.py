@@ -102,6 +102,23 @@ def test_against_the_definition(b, r, c, dtype):
     check(host(g), o, scale=0.7, dtype=dtype)
 
 
+@pytest.mark.parametrize("b,r,c", [(1, 64, 5000), (2, 3000, 200), (3, 100, 2000), (1, 1500, 1530), (2, 1500, 1530), (40, 200, 700), (70, 160, 520), (100, 200, 260),
+                                   (200, 200, 260), (300, 64, 300)])
+def test_every_width_of_tiles(b, r, c):
+    """Contractions dealt to several workgroups; tiles 64, 128 (one and two groups of waves) and 256 wide, in the symmetric products and the others.
+    The first, the last and some of the matrices between."""
+    rng = np.random.default_rng(b + r + c)
+    g = dev(gradient(rng, b, r, c), 0)
+    o = torch.full_like(g, float("nan"))
+    run(g, o)
+    some = sorted({0, b // 3, b // 2, b - 2 if b > 1 else 0, b - 1})
+    check(host(g[some]), o[some])
+    assert torch.isfinite(o).all()
+    again = torch.full_like(g, float("nan"))
+    run(g, again)
+    assert torch.equal(o, again)
+
+
 @pytest.mark.parametrize("noise", [0.0, 1e-4, 1e-2])
 def test_strong_directions_over_noise(noise):
     """Singular values that five steps bring up from nearly nothing, and a matrix of rank 4."""
