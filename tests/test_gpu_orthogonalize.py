@@ -103,7 +103,7 @@ def test_against_the_definition(b, r, c, dtype):
 
 
 @pytest.mark.parametrize("b,r,c", [(1, 64, 5000), (2, 3000, 200), (3, 100, 2000), (1, 1500, 1530), (2, 1500, 1530), (40, 200, 700), (70, 160, 520), (100, 200, 260),
-                                   (200, 200, 260), (300, 64, 300)])
+                                   (200, 200, 260), (300, 64, 300), (9, 900, 1000)])
 def test_every_width_of_tiles(b, r, c):
     """Contractions dealt to several workgroups; tiles 64, 128 (one and two groups of waves) and 256 wide, in the symmetric products and the others.
     The first, the last and some of the matrices between."""
