@@ -771,8 +771,9 @@ static hipError_t ns_launch_small(hipStream_t s, dim3 grid, const NsParams& p, c
 // of waves where there is a workgroup a CU, else to two (one matrix of 1024 x 1024: four groups 197 us, two 213, one 247).  More of
 // them would take a second round: then 128 wide ones, in two groups where each CU has one (2048 x 2048: 64 wide 904 us, 128 wide in two groups
 // 791, in one 1071; six of 1024 x 1024: 64 wide 581, 531, 649), in one where each CU has more (24 of 768 x 2048: 1721, 1587, 1542);
-// A few more 128 wide tiles than CUs would take twice the time of one: 64 wide again (four of 1344 x 1792, 264 tiles: 1028 us against 1153;
-// 325 tiles of 3200 x 3200: 2608 against 2448).  256 wide tiles where they fill the chip (24 of 1024 x 4096: 128 wide 4.4 ms, 3.7), and for
+// for a symmetric product with a few more of them than CUs, which would take twice the time of one, 64 wide again (four of 1344 x 1792, 264
+// tiles: 1028 us against 1153; 325 tiles of 3200 x 3200: 2608 against 2448; but of the products with X, 272 tiles of four of 2100 x
+// 410: 236 against 221).  256 wide tiles where they fill the chip (24 of 1024 x 4096: 128 wide 4.4 ms, 3.7), and for
 // the products with X, which write most, from 144 on (160 of 2500 x 4000: 1720 -> 1481 us; 128 of eight of 1024 x 1024: 736 -> 762;
 // symmetric, 144 of 24 of 768 x 2048: 1542 -> 1692).  No tile is more than twice as wide as a matrix is high.
 template <int KIND, typename T>
@@ -782,7 +783,7 @@ static hipError_t ns_product(hipStream_t s, const NsParams& p, NsProduct q, int 
   int edge = 128;
   if (tiles(64) <= 512 || q.rows_a <= 64) edge = 64;
   else if (q.rows_a > 128 && tiles(256) >= (symmetric ? 192 : 144)) edge = 256;
-  else if (tiles(128) > 256 && tiles(128) <= 300) edge = 64;
+  else if (symmetric && tiles(128) > 256 && tiles(128) <= 300) edge = 64;
   q.tiles = (int)ns_tiles(edge, q.rows_a, q.rows_b, symmetric);
   q.tiles_b = symmetric ? 0 : (q.rows_b + edge - 1) / edge;
   // A workgroup a CU at most, whose share of the contraction costs it what the sums of the other shares cost the one that adds them up: n K-tiles at
