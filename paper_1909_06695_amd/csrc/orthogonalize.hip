@@ -15,6 +15,9 @@
 // 2.0 -> 1.4 ms).  It is as accurate: errors of A' are absolute, 2^-22 |A|, and reach X through C' as 1e-6 of a.  Three steps without X
 // would not be: negative rounding noise in the small eigenvalues of A grows by a^2 a step.
 //
+// Bound by the matrix instructions where matrices are large: 24 of 1024 x 4096, five steps, 3.72 ms, three times 1.21 TFLOP at 0.98 PFLOP/s (a large
+// fp16 product reaches 1.02); by the latency of 17 dependent products where they are small (four of 2100 x 410: 222 us).
+//
 // All products are of the form L R^T with the contraction contiguous in both: X X^T; products of two of the symmetric matrices; and one of
 // those times X^T, for which X is kept in both layouts.  Of the symmetric results only the tiles on and below the diagonal are formed, and
 // stored twice.  Matrices are the smaller dimension times the larger, padded with zeros to whole multiples of 64: zero rows and columns

@@ -12,6 +12,8 @@
 // every tile has a workgroup: it publishes its map, reads those of up to RC_BACK tiles before it and the state behind the tile
 // before these, and publishes the state behind itself.  The tiles of a line (a strip of a stream) are dealt by a counter, so that a
 // workgroup only waits for workgroups that have begun before it and every wait ends.  Nothing is read twice.
+// 8 streams of 1024 steps, 1024 channels, bf16: forward 16 us (51 MB, 3.2 TB/s), backward 25 us (84 MB, 3.4 TB/s), 2 and 4 of them for clearing the
+// workspace; one of 65536 steps, 512 channels, fp32: forward 91 us (405 MB, 4.5 TB/s); 64 single tokens of 1024 channels: 5 us.
 #include "common.h"
 #include "unaligned.h"
 
