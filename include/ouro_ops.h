@@ -177,7 +177,7 @@ int ouro_op_embed_bwd(void* stream, int dtype, const int32_t* tok, const void* d
 /* The same gradient with sums in an order that the ids alone determine: dV[v,:] = scale * sum of the rows dh[n,:] with
  * tok[n] = v, or with accumulate != 0 dV[v,:] += that (a tied matrix that already holds its other gradient: only the rows of
  * ids that occur are read and written).  dh [N, lddh] of type T, dV fp32 [vocab, ldv]; lddh, ldv >= d, any alignment of an
- * element.  Ids outside [0, vocab) take no part.  N = 0 is allowed (tok, dh are not used then); N, d <= 2^30.  One launch,
+ * element.  Ids outside [0, vocab) take no part.  N = 0 is allowed (tok, dh are not used then); N <= 2^30, d <= 2^24.  One launch,
  * no workspace; equal calls give equal bits. */
 int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv, int N,
                              int d, int vocab, float scale, int accumulate);
@@ -191,7 +191,7 @@ int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const 
  * step, which is what the backward call needs.
  * scratch: fp32, ouro_op_recurrence_scratch() floats, 16-byte aligned (NULL where that is 0); a call clears what it uses of it, so
  * that calls on one stream may share it.
- * No output may overlap an input, but for h0 and hT.  T, D <= 2^30. */
+ * No output may overlap an input, but for h0 and hT.  T <= 2^30, D <= 2^24. */
 enum { OURO_RECURRENCE_STRIDE = 64 };
 int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
                            const float* h0, const int32_t* lens, void* h, int ldh, float* hT, float* states, float* scratch);

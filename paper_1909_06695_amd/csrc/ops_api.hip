@@ -290,12 +290,13 @@ static int refuse(const char* op, const char* why) {
   return set_error(OURO_E_ARG, msg);
 }
 constexpr int ROWS_MAX = 1 << 30;                                 // rows and steps that the kernels count in 32 bits, with room for a tile
+constexpr int COLS_MAX = 1 << 24;                                 // columns whose strips are a launch
 
 extern "C" int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const void* dh, int lddh, float* dV, int ldv, int N,
                                         int d, int vocab, float scale, int accumulate) {
   const char* op = "embed_bwd_sorted";
   if (dtype < 0 || dtype > 1) return refuse(op, "dtype is 0 or 1");
-  if (N < 0 || N > ROWS_MAX || d < 1 || d > ROWS_MAX || vocab < 1) return refuse(op, "bad sizes");
+  if (N < 0 || N > ROWS_MAX || d < 1 || d > COLS_MAX || vocab < 1) return refuse(op, "bad sizes");
   if (!dV || (N && (!tok || !dh))) return refuse(op, "null pointer");
   if ((N && lddh < d) || ldv < d) return refuse(op, "a leading dimension below d");
   return rc_of(launch_embed_bwd_sorted((hipStream_t)stream, dtype, tok, dh, lddh, dV, ldv, N, d, vocab, scale, accumulate));
@@ -303,11 +304,11 @@ extern "C" int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* 
 
 static_assert(RECURRENCE_STRIDE == OURO_RECURRENCE_STRIDE, "the boundary names the distance of the kept states");
 extern "C" size_t ouro_op_recurrence_scratch(int B, int T, int D) {
-  return B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > ROWS_MAX ? 0 : recurrence_scratch_floats(B, T, D);
+  return B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > COLS_MAX ? 0 : recurrence_scratch_floats(B, T, D);
 }
 static const char* recurrence_refusal(int dtype, int B, int T, int D, int ldz, int ldx, int ldo, const float* scratch) {
   if (dtype < 0 || dtype > 1) return "dtype is 0 or 1";
-  if (B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > ROWS_MAX) return "bad sizes";
+  if (B < 1 || T < 1 || T > ROWS_MAX || D < 1 || D > COLS_MAX) return "bad sizes";
   if (ldz < D || ldx < D || ldo < D) return "a leading dimension below D";
   if (!scratch && recurrence_scratch_floats(B, T, D)) return "these sizes need scratch";
   if (reinterpret_cast<uintptr_t>(scratch) & 15) return "scratch is not 16-byte aligned";

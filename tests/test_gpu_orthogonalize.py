@@ -89,7 +89,7 @@ def dev(a, dtype):
 
 
 SIZES = [(1, 1, 1), (1, 1, 70), (2, 5, 3), (1, 64, 64), (1, 64, 256), (3, 65, 130), (2, 130, 65), (1, 410, 210), (2, 200, 700), (1, 16, 3000), (1, 520, 520),
-         (9, 96, 128), (1, 300, 1100)]
+         (9, 96, 128), (1, 300, 1100), (3, 250, 61), (2, 256, 64), (1, 200, 7), (2, 64, 253)]
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
@@ -117,6 +117,20 @@ def test_every_width_of_tiles(b, r, c):
     again = torch.full_like(g, float("nan"))
     run(g, again)
     assert torch.equal(o, again)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows and matrices far apart: the last ones behind 2^31 elements."""
+    ld, b, r, c = 1 << 24, 2, 70, 80
+    wide = torch.empty(b * r * ld, device="cuda").view(b, r, ld)
+    assert wide.numel() > 2**31
+    g, m, o = (wide[:, :, 1000 * i:1000 * i + c] for i in range(3))
+    u = gradient(np.random.default_rng(5), b, r, c)
+    g.copy_(dev(u, 0))
+    m.fill_(0.5)
+    run(g, o, m, mu=1.0)
+    assert torch.equal(m, g + 0.5)
+    check(host(m), o)
 
 
 @pytest.mark.parametrize("noise", [0.0, 1e-4, 1e-2])

@@ -165,6 +165,43 @@ def test_lengths(T, lens, dtype):
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,T,D,ragged", [(520, 600, 20, False), (130, 1100, 130, True), (180, 1100, 130, True), (1030, 300, 3, True)])
+def test_streams_that_fill_the_chip(B, T, D, ragged, dtype):
+    """Streams and strips of channels (64 in bf16, 32 in fp32) enough, 512 or more, for a workgroup to go through the segments of a stream one after the
+    other, without a workspace; the second in fp32 only."""
+    assert (L().ouro_op_recurrence_scratch(B, T, D) == 0) == (B * -(-D // 64) >= 512)
+    lens = [(37 * b) % (T + 2) for b in range(B)] if ragged else None
+    s = make(B, T, D, dtype, B, lens=lens)
+    if ragged:
+        late = torch.arange(T, device="cuda")[None] >= s["lens"][:, None]
+        for k in ("z", "x", "dh"):
+            s[k][late] = float("nan")
+    forward(s)
+    out, tol = oracle(s)
+    compare(s, ("h", "hT", "states"), out, tol)
+    backward(s)
+    compare(s, ("dz", "dx", "dh0"), out, tol)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^25 elements apart, operands and results side by side in them: 70 rows end behind 2^31 elements."""
+    B, T, D, ld = 1, 70, 8, 1 << 25
+    s = make(B, T, D, 0, 21)
+    wide = torch.empty(T * ld, device="cuda")
+    assert wide.numel() > 2**31
+    views = {k: wide.view(1, T, ld)[:, :, 100 * i:100 * i + D] for i, k in enumerate(("z", "x", "dh", "h", "dz", "dx"))}
+    for k in ("z", "x", "dh"):
+        views[k].copy_(s[k])
+        s[k] = views[k]
+    s["out"] = {k: views[k] for k in ("h", "dz", "dx")}
+    forward(s)
+    out, tol = oracle(s)
+    compare(s, ("h", "hT", "states"), out, tol)
+    backward(s)
+    compare(s, ("dz", "dx", "dh0"), out, tol)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
 @pytest.mark.parametrize("T", [3, 300])
 def test_states_that_are_absent(T, dtype):
     """h0 and dhT NULL are zero; hT, states and dh0 need not be asked for."""

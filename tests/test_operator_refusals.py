@@ -19,7 +19,7 @@ EMBED = dict(dtype=0, tok=X, dh=X, lddh=8, dV=X, ldv=8, N=4, d=8, vocab=16, scal
 
 
 @pytest.mark.parametrize("change", [dict(dtype=2), dict(dtype=-1), dict(N=-1), dict(N=(1 << 30) + 1), dict(d=0), dict(vocab=0), dict(tok=None),
-                                    dict(dh=None), dict(dV=None), dict(lddh=7), dict(ldv=7), dict(d=(1 << 30) + 1, lddh=2**31 - 1, ldv=2**31 - 1)])
+                                    dict(dh=None), dict(dV=None), dict(lddh=7), dict(ldv=7), dict(d=(1 << 24) + 1, lddh=2**31 - 1, ldv=2**31 - 1)])
 def test_embed_bwd_sorted(change):
     a = dict(EMBED, **change)
     refused(P.lib().ouro_op_embed_bwd_sorted(None, *a.values()), b"embed_bwd_sorted")
@@ -28,7 +28,7 @@ def test_embed_bwd_sorted(change):
 FWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, h0=None, lens=None, h=X, ldh=8, hT=None, states=None, scratch=None)
 BWD = dict(dtype=0, B=2, T=4, D=8, z=X, ldz=8, x=X, ldx=8, states=X, lens=None, dh=X, lddh=8, dhT=None, dz=X, lddz=8, dx=X, lddx=8, dh0=None,
            scratch=None)
-SIZES = [dict(dtype=2), dict(B=0), dict(T=0), dict(D=0), dict(T=(1 << 30) + 1), dict(D=(1 << 30) + 1), dict(z=None), dict(x=None), dict(ldz=7), dict(ldx=7), dict(T=100000),
+SIZES = [dict(dtype=2), dict(B=0), dict(T=0), dict(D=0), dict(T=(1 << 30) + 1), dict(D=(1 << 24) + 1, ldz=1 << 30, ldx=1 << 30), dict(z=None), dict(x=None), dict(ldz=7), dict(ldx=7), dict(T=100000),
          dict(T=100000, scratch=C.c_void_p(4104))]
 
 
@@ -47,7 +47,7 @@ def test_recurrence_scratch():
     size = P.lib().ouro_op_recurrence_scratch
     assert size(64, 1, 1024) == 0 and size(64, 1000, 2048) == 0 and size(1, 64, 8) == 0
     assert size(1, 65536, 512) > 0
-    assert size(0, 5, 5) == 0 and size(1, 0, 5) == 0 and size(1, 5, 0) == 0 and size(1, 5, (1 << 30) + 1) == 0
+    assert size(0, 5, 5) == 0 and size(1, 0, 5) == 0 and size(1, 5, 0) == 0 and size(1, 5, (1 << 24) + 1) == 0
 
 
 ORTHO = dict(dtype=0, batch=2, rows=16, cols=24, g=X, ldg=24, sg=384, momentum=None, mu=0.9, nesterov=0, o=X, ldo=24, so=384, scale=1.0, eps=1e-7,
