@@ -27,6 +27,8 @@ constexpr int ES_COUNT = 128;                              // longest list that 
                                                            // against 3.5 from runs)
 constexpr int ES_BITS = 9, ES_BINS = 1 << ES_BITS;         // largest digit of the radix sort
 constexpr int ES_ROW_BITS = 14;                            // matrix rows of a workgroup: a bit each, two digits
+constexpr int ES_HOT = 4096;                               // ids of one token from which on they are summed without a list, looked for among more than four times as many
+                                                           // (looking takes 2 us; 60 % of 32768 ids, 1024 columns in fp32: 148 -> 77 us, bf16 245 -> 157; of 16384: as before)
 constexpr int ES_COLD_COST = 3;                            // rows summed in the time of one that is a sum by itself
 constexpr int ES_CLEARERS = 256;                           // workgroups that clear rows, one a CU
 static_assert(ES_BINS == ES_THREADS, "one bin a thread");
@@ -96,6 +98,73 @@ __device__ __forceinline__ void es_clear(const EmbedSortedParams& p, uint32_t z0
   }
 }
 
+// A token of the workgroup's rows that makes up ES_HOT ids and more by a sample of 64 of them, or -1 (every wave finds the same).
+__device__ __forceinline__ int es_hot(const EmbedSortedParams& p, uint32_t R, uint32_t mine) {
+  const int lane = threadIdx.x & 63, id = p.tok[(long)lane * p.N / 64];
+  const bool on = (uint32_t)id < (uint32_t)p.vocab && ((uint32_t)id & (R - 1)) == mine;
+  uint32_t best = (uint32_t)__popcll(es_peers((uint32_t)id, 31, __ballot(on))) << 6 | (uint32_t)lane;
+  if (!on) best = 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o, 64));
+  const int hot = __shfl(id, (int)(best & 63), 64);
+  return (long)(best >> 6) * p.N >= 64l * ES_HOT ? __builtin_amdgcn_readfirstlane(hot) : -1;
+}
+// This lane's columns of the sum of the rows of token `hot`: each wave goes through its ids and sums the rows as it finds them, eight at a
+// time a team.  `list`: the wave's, ES_WAVE_CAP entries; the sums of the teams are left in `heads`.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void es_sum_hot(const EmbedSortedParams& p, const LaneColumns& own, int hot, int wave, uint32_t* list, float* heads) {
+  constexpr int P = 16 / sizeof(T), U = 8, ROUND = U * 64 / STRIP_LANES;
+  static_assert(ES_WAVE_CAP >= 2 * ES_STEP + ROUND, "what is left of a round and two steps");
+  const int lane = threadIdx.x & 63, team = lane / STRIP_LANES;
+  const T* dh = reinterpret_cast<const T*>(p.dh) + own.col;
+  float acc[P] = {};
+  int4 v[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) v[u] = es_ids(p, (wave * 2 + u) * ES_STEP + 4 * lane);
+  int k = 0;
+  for (int n = wave * 2 * ES_STEP; n < p.N; n += ES_WAVES * 2 * ES_STEP) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      auto take = [&](int id, int at) __attribute__((always_inline)) {
+        const uint64_t all = __ballot(id == hot);
+        if (id == hot) list[k + es_below(all)] = (uint32_t)at;
+        k += (int)__popcll(all);
+      };
+      const int at = n + u * ES_STEP + 4 * lane;
+      take(v[u].x, at); take(v[u].y, at + 1); take(v[u].z, at + 2); take(v[u].w, at + 3);
+      v[u] = es_ids(p, at + ES_WAVES * 2 * ES_STEP);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const bool last = n + ES_WAVES * 2 * ES_STEP >= p.N;
+    int r = 0;
+    for (; r + ROUND <= k; r += ROUND) {
+      UnalignedPack<T, P> x[U] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_raw_columns<T, P, WHOLE>(dh + (size_t)list[r + u * (64 / STRIP_LANES) + team] * p.lddh, x[u], own.n);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < P; ++j) acc[j] += to_f32(x[u].v[j]);
+    }
+    if (last) {
+      for (int i = r + team; i < k; i += 64 / STRIP_LANES) {
+        UnalignedPack<T, P> x = {};
+        load_raw_columns<T, P, WHOLE>(dh + (size_t)list[i] * p.lddh, x, own.n);
+#pragma unroll
+        for (int j = 0; j < P; ++j) acc[j] += to_f32(x.v[j]);
+      }
+    } else if (r > 0) {                                    // what is left, to the front
+      k -= r;
+      const uint32_t e = lane < k ? list[r + lane] : 0;
+      __builtin_amdgcn_wave_barrier();
+      if (lane < k) list[lane] = e;
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < P; ++j) heads[(wave * (64 / STRIP_LANES) + team) * STRIP_LANES * P + lane % STRIP_LANES * P + j] = acc[j];
+}
+
 // WHOLE: see lane_columns.  ADD: onto what the matrix holds.
 template <typename T, bool WHOLE, bool ADD>
 __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSortedParams p) {
@@ -118,6 +187,25 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
   const int team = tid / STRIP_LANES;
   for (int i = tid; i < 1 << max(0, p.row_bits - 5); i += ES_THREADS) seen[i] = 0;
 
+  // ---- a token of very many ids: no list holds them, and its rows come in any order
+  const int hot = p.N > 4 * ES_HOT ? es_hot(p, R, mine) : -1;
+  if (hot >= 0) {
+    float* heads = reinterpret_cast<float*>(hist_or_heads);
+    es_sum_hot<T, WHOLE>(p, own, hot, wave, list_a + wave * ES_WAVE_CAP, heads);
+    __syncthreads();
+    if (team == 0) {
+      float acc[P] = {}, old[P] = {};
+      float* out = p.dV + (size_t)hot * p.ldv + own.col;
+      if (ADD) load_columns<float, P, WHOLE>(out, old, own.n);
+      for (int t = 0; t < ES_TEAMS; ++t)
+#pragma unroll
+        for (int j = 0; j < P; ++j) acc[j] += heads[t * W + lane * P + j];
+#pragma unroll
+      for (int j = 0; j < P; ++j) old[j] = fmaf(p.scale, acc[j], old[j]);
+      store_columns<float, P, WHOLE>(out, old, own.n);
+    }
+  }
+
   bool first = true, end = false;
   int n0 = 0;                                              // ids before n0 have been looked at
   while (!end) {
@@ -138,7 +226,7 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
         if (full) continue;
         const int at = gone + wave * ES_STEP + 4 * lane;
         auto take = [&](uint32_t id, int n) __attribute__((always_inline)) {
-          const bool on = id < (uint32_t)p.vocab && (id & (R - 1)) == mine;
+          const bool on = id < (uint32_t)p.vocab && (id & (R - 1)) == mine && (int)id != hot;
           const uint64_t all = __ballot(on);
           if (on) list_a[wave * ES_WAVE_CAP + k + es_below(all)] = id >> p.log2R << p.n_bits | (uint32_t)n;
           k += (int)__popcll(all);

@@ -146,6 +146,29 @@ def test_offsets_beyond_32_bits():
 
 
 @pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("N,vocab,d,shares", [(20000, 1000, 130, (0.9, 0.05)), (20001, 40, 3, (0.5, 0.45)), (4096, 9, 64, (1.0, 0.0)), (16385, 9, 64, (1.0, 0.0)), (40000, 100, 7, (0.2, 0.6)), (30000, 50000, 410, (0.3, 0.3)),
+                                              (12345, 2, 33, (0.5, 0.5))])
+def test_tokens_that_no_list_holds(N, vocab, d, shares, dtype, accumulate):
+    """One token and two of thousands of ids, on rows off every alignment; equal calls give equal bits."""
+    rng = np.random.default_rng(N + d)
+    tok, dh = case(rng, N, vocab, d, dtype, outside=0.02)
+    u = rng.random(N)
+    tok[u < shares[0]] = vocab - 1
+    tok[(u >= shares[0]) & (u < sum(shares))] = vocab // 2
+    wide = torch.zeros(N, d + 5, dtype=dh.dtype, device="cuda")[:, 2:2 + d]
+    wide.copy_(dh)
+    old = rng.standard_normal((vocab, d)).astype(np.float32)
+    got = []
+    for _ in range(2):
+        out = torch.from_numpy(old).cuda()
+        ok(L().ouro_op_embed_bwd_sorted(stream(), dtype, p(torch.from_numpy(tok).cuda()), p(wide), d + 5, p(out), d, N, d, vocab, 1.5, accumulate))
+        got.append(out)
+    check(tok, dh, got[0].double().cpu().numpy(), accumulate, vocab, 1.5, old)
+    assert torch.equal(got[0], got[1])
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
 def test_the_largest_vocabulary(accumulate):
     """2^31 - 1 rows of one column: the first, the last and one of a later workgroup's; everything else is cleared, or left as it was."""
     vocab = 2**31 - 1
