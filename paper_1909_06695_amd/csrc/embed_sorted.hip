@@ -4,11 +4,11 @@
 // One launch, no workspace, no atomics on memory.  A workgroup owns the matrix rows v with v mod R = r and 128 bytes of
 // columns of dh.  It reads all N ids (they stay in L2), keeps those of its rows as a list in LDS, sorts the list by row with a
 // stable sort, and its teams of 8 lanes (16 bytes each) sum equal pieces of the sorted list: a frequent token is summed by
-// many teams, whose parts are joined in order through LDS.  Every sum therefore has an order that only the ids determine.
+// many teams, whose parts are joined in order through LDS; one of thousands of ids is summed without a list.  Every sum therefore has an order that only the ids determine.
 // Rows are dealt to workgroups by v mod R because ids are usually ranked by frequency: neighbours are alike in weight.
 //
 // Bound by memory: N d elements read, the matrix written (or the rows of tokens that occur read and written).  8192 ids, 32768 x 512 in
-// fp32: 21 us (84 MB, 4.0 TB/s); 4800 ids, 32768 x 410 in bf16: 22.5 us (58 MB).  Where one token makes up much of the ids, by the workgroups
+// fp32: 21 us (84 MB, 4.0 TB/s); 4800 ids, 32768 x 410 in bf16: 23 us (58 MB).  Where one token makes up much of the ids, by the workgroups
 // that own its row, at about 12 bytes/ns each (the lines a CU has under way): 8192 ids, a quarter of them one token, added to 50257 x
 // 1024: 25 us (50 MB), 9 of which go to finding and sorting the entries.  Without a workspace no others can share them.
 #include "common.h"
