@@ -4,8 +4,9 @@
 // One launch, no workspace, no atomics on memory.  A workgroup owns the matrix rows v with v mod R = r and 128 bytes of
 // columns of dh.  It reads all N ids (they stay in L2), keeps those of its rows as a list in LDS, sorts the list by row with a
 // stable sort, and its teams of 8 lanes (16 bytes each) sum equal pieces of the sorted list: a frequent token is summed by
-// many teams, whose parts are joined in order through LDS; one of thousands of ids is summed without a list.  Every sum therefore has an order that only the ids determine.
-// Rows are dealt to workgroups by v mod R because ids are usually ranked by frequency: neighbours are alike in weight.
+// many teams, whose parts are joined in order through LDS; one of thousands of ids is summed without a list.  Every sum therefore
+// has an order that only the ids determine.  Rows are dealt to workgroups by v mod R because ids are usually ranked by frequency:
+// neighbours are alike in weight.
 //
 // Bound by memory: N d elements read, the matrix written (or the rows of tokens that occur read and written).  8192 ids, 32768 x 512 in
 // fp32: 21 us (84 MB, 4.0 TB/s); 4800 ids, 32768 x 410 in bf16: 23 us (58 MB).  Where one token makes up much of the ids, by the workgroups
@@ -27,8 +28,9 @@ constexpr int ES_COUNT = 128;                              // longest list that 
                                                            // against 3.5 from runs)
 constexpr int ES_BITS = 9, ES_BINS = 1 << ES_BITS;         // largest digit of the radix sort
 constexpr int ES_ROW_BITS = 14;                            // matrix rows of a workgroup: a bit each, two digits
-constexpr int ES_HOT = 4096;                               // ids of one token from which on they are summed without a list, looked for among more than four times as many
-                                                           // (looking takes 2 us; 60 % of 32768 ids, 1024 columns in fp32: 148 -> 77 us, bf16 245 -> 157; of 16384: as before)
+constexpr int ES_HOT = 4096;                               // ids of one token from which on they are summed without a list, looked for among more than
+                                                           // four times as many (looking takes 2 us; 60 % of 32768 ids, 1024 columns, fp32: 148 -> 77 us,
+                                                           // bf16: 245 -> 157; of 16384: as before)
 constexpr int ES_COLD_COST = 3;                            // rows summed in the time of one that is a sum by itself
 constexpr int ES_CLEARERS = 256;                           // workgroups that clear rows, one a CU
 static_assert(ES_BINS == ES_THREADS, "one bin a thread");
