@@ -223,7 +223,8 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
       for (int u = 0; u < AHEAD; ++u) {
         end = n0 >= p.N;
         const int gone = n0 - n_base;
-        full = full || end || gone > (1 << p.n_bits) - ES_WAVES * ES_STEP;
+        // (a step before the positions end: no entry has all bits set, which stands for none where runs are sorted)
+        full = full || end || gone >= (1 << p.n_bits) - ES_WAVES * ES_STEP;
         if (!full && gone >= ES_WAVES * ES_WAVE_CAP) full = __syncthreads_or(k > ES_WAVE_CAP - ES_STEP);
         if (full) continue;
         const int at = gone + wave * ES_STEP + 4 * lane;

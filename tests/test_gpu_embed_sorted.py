@@ -182,3 +182,44 @@ def test_the_largest_vocabulary(accumulate):
         out[at] = accumulate
     step = 1 << 28
     assert all((out[i:i + step] == accumulate).all() for i in range(0, vocab, step))
+
+
+def last_of_positions(N, vocab, d, dtype, accumulate, per_class, classes, more=0):
+    """Ids of which the last of N is the last of the vocabulary, `per_class` on average those of each of `classes` residues, the others outside the
+    vocabulary; `more` ids behind them.
+
+    An entry has N positions at most, and ids behind them are summed after those before: a row that occurs in w such parts gets w sums, each by
+    one fma, and each rounds by at most 2^-24 of what the element is then, at most |old| + the sum of magnitudes (|old| is 0 where the matrix is
+    written).  The other roundings are those of any sum of k terms, as above.  No list is full before its positions end: it holds 768 entries of each
+    of 8 waves, and a class has fewer than 1200 in all."""
+    rng = np.random.default_rng(per_class + more)
+    tok, dh = case(rng, N + more, vocab, d, dtype)
+    tok[rng.random(N + more) >= per_class * classes / N] = -1
+    tok[N - 1] = vocab - 1
+    old = rng.standard_normal((vocab, d)).astype(np.float32)
+    out = torch.from_numpy(old).cuda() if accumulate else torch.full((vocab, d), float("nan"), device="cuda")
+    ok(L().ouro_op_embed_bwd_sorted(stream(), dtype, p(torch.from_numpy(tok).cuda()), p(dh), d, p(out), d, N + more, d, vocab, 0.5, accumulate))
+    x, inside = 0.5 * dh.double().cpu().numpy(), tok >= 0
+    ref, mag, k = np.zeros((vocab, d)), np.zeros((vocab, d)), np.zeros((vocab, 1))
+    np.add.at(ref, tok[inside], x[inside])
+    np.add.at(mag, tok[inside], np.abs(x[inside]))
+    np.add.at(k, tok[inside], 1)
+    w = -(-(N + more) // (N - 2048))                             # (a step of 2048 ids before the positions end begins another part)
+    base = old.astype(np.float64) if accumulate else np.zeros((vocab, d))
+    assert np.all(np.abs(out.double().cpu().numpy() - (base + ref)) <= 2.0 ** -24 * ((k + 1) * mag + w * (np.abs(base) + mag)))
+
+
+# 2^22 rows go to 2^8 workgroups (2^9 where the sums are added): 14 (13) bits of an entry are the row and 18 (19) the position, and the last id of
+# 2^18 (2^19) at the last row would be an entry of ones.
+@pytest.mark.parametrize("per_class", [60, 150, 400, 900])
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_the_last_row_at_the_last_position(accumulate, dtype, per_class):
+    """Lists that are sorted by counting, from runs and by radix."""
+    last_of_positions(1 << (18 + accumulate), 1 << 22, 8 if dtype else 4, dtype, accumulate, per_class, 256 << accumulate)
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("more", [1, 3000, 300000])
+def test_more_ids_than_an_entry_has_positions(more, accumulate):
+    last_of_positions(1 << (18 + accumulate), 1 << 22, 4, 0, accumulate, 300, 256 << accumulate, more)
