@@ -460,8 +460,7 @@ hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r) 
   const bool backward = r.dz != nullptr;
   const RcPlan plan = rc_plan(dtype, backward, r.B, r.T, r.D);
   const bool chained = plan.mode == RC_CHAINED;
-  const long long blocks = (long long)r.B * plan.strips * (chained ? plan.tiles : 1);
-  if (blocks * 64 * plan.waves >> 32 || (chained && !r.scratch)) return hipErrorInvalidValue;
+  if (chained && !r.scratch) return hipErrorInvalidValue;
   RecurrenceParams p;
   memset(&p, 0, sizeof p);
   p.B = r.B; p.T = r.T; p.D = r.D; p.strips = plan.strips; p.tiles = plan.tiles;
@@ -477,9 +476,29 @@ hipError_t launch_recurrence(hipStream_t s, int dtype, const RecurrenceDesc& r) 
     const hipError_t e = launch_fill_zero(s, at, rc_scratch_bytes(plan, r.B, r.D));
     if (e != hipSuccess) return e;
   }
-  if (dtype == 1) r.D >= RC_P ? rc_launch<bf16_t, true>(s, (unsigned)blocks, plan, p, backward) : rc_launch<bf16_t, false>(s, (unsigned)blocks, plan, p, backward);
-  else r.D >= RC_P ? rc_launch<float, true>(s, (unsigned)blocks, plan, p, backward) : rc_launch<float, false>(s, (unsigned)blocks, plan, p, backward);
-  return hipGetLastError();
+  // A grid has less than 2^32 work items: the tiles of chained lines go into as many launches as that takes, in which the tickets go on
+  // (one stream of 2^30 steps in bf16, backward: 2^23 tiles of 512 threads), and so do the streams of the others.
+  const long long most = ((1ll << 32) - 1) / (64 * plan.waves);            // workgroups of a launch
+  const long long all = chained ? plan.tiles : r.B, per = std::min(all, most / ((long long)plan.strips * (chained ? r.B : 1)));
+  const size_t e = dtype == 1 ? 2 : 4, chunks = ((size_t)r.T + RC_KEEP - 1) / RC_KEEP;
+  for (long long at = 0; at < all; at += per) {
+    RecurrenceParams q = p;
+    const long long n = std::min(per, all - at);
+    if (!chained) {
+      q.B = (int)n;
+      const size_t row = (size_t)at * r.T, state = (size_t)at * r.D;
+      auto rows = [&](auto*& of, size_t ld) { if (of) of = (char*)of + row * ld * e; };
+      auto states = [&](auto*& of, size_t apart) { if (of) of += apart; };
+      rows(q.z, q.ldz); rows(q.x, q.ldx); rows(q.dh, q.lddh); rows(q.h, q.ldh); rows(q.dz, q.lddz); rows(q.dx, q.lddx);
+      states(q.h0, state); states(q.hT, state); states(q.dhT, state); states(q.dh0, state); states(q.states, state * chunks); states(q.lens, at);
+    }
+    const unsigned blocks = (unsigned)(n * plan.strips * (chained ? r.B : 1));
+    if (dtype == 1) r.D >= RC_P ? rc_launch<bf16_t, true>(s, blocks, plan, q, backward) : rc_launch<bf16_t, false>(s, blocks, plan, q, backward);
+    else r.D >= RC_P ? rc_launch<float, true>(s, blocks, plan, q, backward) : rc_launch<float, false>(s, blocks, plan, q, backward);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ouro

@@ -10,7 +10,7 @@
 #include <vector>
 
 struct dim3 { unsigned x, y, z; };
-struct Launch { std::string name; int first_arg; };
+struct Launch { std::string name; int first_arg; unsigned blocks; };
 static std::map<const void*, std::string>& names() { static auto* n = new std::map<const void*, std::string>; return *n; }
 static std::vector<Launch>& log_() { static auto* l = new std::vector<Launch>; return *l; }
 static int fail_from = -1, fail_times = 0, last_error = 0;
@@ -29,6 +29,7 @@ void fake_reset() { log_().clear(); }
 int fake_count() { return (int)log_().size(); }
 const char* fake_name(int i) { return log_()[i].name.c_str(); }
 int fake_first_arg(int i) { return log_()[i].first_arg; }               // the first int of the kernel's first argument
+unsigned fake_blocks(int i) { return log_()[i].blocks; }                 // along x
 void fake_fail(int from, int times) { fail_from = from; fail_times = times; }
 long fake_news(int on) { const long n = news; news = 0; counting = on != 0; return n; }
 
@@ -50,7 +51,7 @@ int hipLaunchKernel(const void* f, dim3 g, dim3 b, void** args, size_t, void*) {
   counting = false;
   int a;
   memcpy(&a, args[0], sizeof a);
-  log_().push_back({names()[f], a});
+  log_().push_back({names()[f], a, g.x});
   counting = was;
   return 0;
 }

@@ -164,6 +164,31 @@ def update_bytes(fake):
         assert n.value == 1 and work.value == want, (dtype, aligned, work.value, want)
 
 
+def recurrences_of_any_length(fake):
+    """The largest sizes that the boundary names: each launch is a grid that there is, and all of them together have a workgroup for every tile and
+    stream."""
+    m = Model(fake)
+    m.F.fake_blocks.restype = C.c_uint
+    m.L.ouro_op_recurrence_scratch.restype = C.c_size_t
+    x = C.c_void_p(256)
+    for dtype, B, T, D, tile_fwd, tile_bwd in ((1, 1, 1 << 30, 1, 256, 128), (0, 1, 1 << 30, 1, 512, 256), (1, 2, 1 << 29, 4, 256, 128), (1, 3, (1 << 30) - 5, 64, 256, 128),
+                                               (1, 500, 1 << 24, 1, 256, 128), (1, 1 << 26, 1, 1, 0, 0), (0, (1 << 31) - 1, 1, 1, 0, 0), (1, 1 << 22, 1000, 40, 0, 0),
+                                               (0, 1, 1, 1 << 24, 0, 0), (1, 70, 1 << 20, 1 << 20, 0, 0)):
+        strips = -(-(-(-D // 4)) // (16 if dtype else 8))
+        for backward, tile in ((0, tile_fwd), (1, tile_bwd)):
+            if backward:
+                rc, log = m.log(lambda: m.L.ouro_op_recurrence_bwd(None, dtype, B, T, D, x, D, x, D, x, None, x, D, None, x, D, x, D, None, x))
+            else:
+                rc, log = m.log(lambda: m.L.ouro_op_recurrence_fwd(None, dtype, B, T, D, x, D, x, D, None, None, x, D, None, None, x))
+            assert rc == 0, (dtype, B, T, D, backward, rc)
+            blocks = [m.F.fake_blocks(i) for i, (name, _) in enumerate(log) if "recurrence" in name]
+            streams = [n for name, n in log if "recurrence" in name]
+            assert sum(blocks) == B * strips * (-(-T // tile) if tile else 1), (dtype, B, T, D, backward, blocks)
+            assert streams == [B] * len(blocks) if tile else sum(streams) == B, (dtype, B, T, D, backward, streams)
+            if tile:                                               # a line gets the same number of workgroups as any other in each launch
+                assert all(n % (B * strips) == 0 for n in blocks)
+
+
 if __name__ == "__main__":
     globals()[sys.argv[2]](sys.argv[1])
     print("passed")

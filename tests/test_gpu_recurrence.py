@@ -340,3 +340,63 @@ def test_streams_and_graphs(dtype):
         backward(s)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, now()))
+
+
+def test_the_longest_stream():
+    """2^30 steps of one channel in bf16, whose 2^23 tiles backward are two launches: windows at the start (the launches meet at step
+    128), in the middle and at the end.  A window's oracle begins 400 steps before it and ends 400 behind it from zeros; what they leave out passes through 400 gates, a factor below 2^-200."""
+    T, wide, far = 1 << 30, 600, 400
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    s = {"B": 1, "T": T, "D": 1, "dtype": 1, "lens": None}
+    for k in ("z", "x", "dh"):
+        s[k] = torch.empty(1, T, 1, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    s["out"] = {k: torch.full_like(s["z"], float("nan")) for k in ("h", "dz", "dx")}
+    s["h0"], s["dhT"] = dev([[2.0]], 0), dev([[-3.0]], 0)
+    s["hT"], s["dh0"] = dev([[5.0]], 0), dev([[5.0]], 0)
+    s["states"] = torch.full((1, T // STRIDE, 1), float("nan"), device="cuda")
+    s["scratch"] = torch.full((L().ouro_op_recurrence_scratch(1, T, 1),), float("nan"), device="cuda")
+    forward(s)
+    backward(s)
+    assert not any(torch.isnan(t).any() for t in (*s["out"].values(), s["states"]))
+    for at in (0, T // 2 + 1, T - wide):
+        lo, hi = max(0, at - far), min(T, at + wide + far)
+        part = {"B": 1, "T": hi - lo, "D": 1, "dtype": 1, "lens": None, "h0": s["h0"] if lo == 0 else torch.zeros(1, 1, device="cuda"),
+                "dhT": s["dhT"] if hi == T else torch.zeros(1, 1, device="cuda")}
+        for k in ("z", "x", "dh"):
+            part[k] = s[k][:, lo:hi]
+        f = 1 / (1 + np.exp(-host(part["z"])[0, :, 0]))
+        assert (lo == 0 or f[:far].prod() < 2.0**-200) and (hi == T or f[-far:].prod() < 2.0**-200)
+        out, tol = oracle(part)
+        for k in ("h", "dz", "dx"):
+            got = host(s["out"][k][:, at:at + wide])
+            assert np.all(np.abs(got - out[k][:, at - lo:at - lo + wide]) <= tol[k][:, at - lo:at - lo + wide]), (k, at)
+        if hi == T:
+            assert abs(s["hT"].item() - out["hT"].item()) <= tol["hT"].item()
+        if lo == 0:
+            assert abs(s["dh0"].item() - out["dh0"].item()) <= tol["dh0"].item()
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_more_streams_than_a_launch(dtype):
+    """2^26 + 5 streams of one token and one channel are two launches; some have no step.  h, dx and dz against the formulas in 64 bits."""
+    B = (1 << 26) + 5
+    gen = torch.Generator(device="cuda").manual_seed(29)
+    ty = torch.bfloat16 if dtype else torch.float32
+    z, x, dh = (torch.empty(B, dtype=ty, device="cuda").normal_(generator=gen) for _ in range(3))
+    h0, dhT = (torch.empty(B, device="cuda").normal_(generator=gen) for _ in range(2))
+    lens = torch.randint(0, 3, (B,), dtype=torch.int32, generator=gen, device="cuda")
+    h, dz, dx = (torch.full_like(z, float("nan")) for _ in range(3))
+    hT, dh0, states = (torch.full_like(h0, float("nan")) for _ in range(3))
+    ok(L().ouro_op_recurrence_fwd(stream(), dtype, B, 1, 1, p(z), 1, p(x), 1, p(h0), p(lens), p(h), 1, p(hT), p(states), None))
+    ok(L().ouro_op_recurrence_bwd(stream(), dtype, B, 1, 1, p(z), 1, p(x), 1, p(states), p(lens), p(dh), 1, p(dhT), p(dz), 1, p(dx), 1, p(dh0), None))
+    assert torch.equal(states, h0)
+    for lo, hi in ((0, 1 << 20), ((1 << 26) - (1 << 20), B)):
+        at = slice(lo, hi)
+        live = host(lens[at]) > 0
+        part = {"B": hi - lo, "T": 1, "D": 1, "dtype": dtype, "lens": lens[at], "h0": h0[at, None], "dhT": dhT[at, None]}
+        part.update(z=z[at, None, None], x=x[at, None, None], dh=dh[at, None, None])
+        out, tol = oracle(part)
+        for got, k in ((h, "h"), (hT, "hT"), (dz, "dz"), (dx, "dx"), (dh0, "dh0")):
+            assert np.all(np.abs(host(got[at]) - out[k].reshape(-1)) <= tol[k].reshape(-1)), k
+        assert not host(h[at])[~live].any()
+    assert not any(torch.isnan(t).any() for t in (h, dz, dx, hT, dh0))

@@ -312,3 +312,7 @@ def test_updates_of_unaligned_matrices(fake_hip):
 
 def test_bytes_of_a_timed_update(fake_hip):
     fake_hip("update_bytes")
+
+
+def test_recurrences_of_any_length_can_be_launched(fake_hip):
+    fake_hip("recurrences_of_any_length")
