@@ -400,3 +400,23 @@ def test_more_streams_than_a_launch(dtype):
             assert np.all(np.abs(host(got[at]) - out[k].reshape(-1)) <= tol[k].reshape(-1)), k
         assert not host(h[at])[~live].any()
     assert not any(torch.isnan(t).any() for t in (h, dz, dx, hT, dh0))
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,T,D", [(1, 200, 16), (2, 1500, 40), (520, 600, 8)])
+def test_a_kept_state_on_the_device(B, T, D, dtype):
+    """Steps with z = +infinity in one tile, over several chained ones and over those that one workgroup goes through: their dz and dx are exactly 0, and h is what it
+    was before them.  Threads and tiles form it from the steps before grouped differently, 32 roundings of at most the largest |h0| and |x| among those for
+    either of the two that are compared, and as T each is off by half a step."""
+    s = make(B, T, D, dtype, T + D)
+    lo, hi = T // 4, T // 4 * 3
+    s["z"][:, lo:hi] = float("inf")
+    forward(s)
+    backward(s)
+    h = host(s["out"]["h"])
+    most = np.maximum(np.abs(host(s["h0"])), np.abs(host(s["x"])[:, :lo]).max(1))
+    tol = 2 * 32 * U * most + HALF[dtype] * (2 * np.abs(h[:, lo - 1]) + 64 * U * most) * (1 + 2 * HALF[dtype])
+    assert np.all(np.abs(h[:, lo:hi] - h[:, lo - 1:lo]) <= tol[:, None])
+    for k in ("dz", "dx"):
+        assert not s["out"][k][:, lo:hi].any(), k
+        assert s["out"][k][:, :lo].any() and s["out"][k][:, hi:].any(), k
