@@ -184,7 +184,9 @@ int ouro_op_embed_bwd_sorted(void* stream, int dtype, const int32_t* tok, const 
 /* Gated linear recurrence over B streams of T steps and D channels: f = sigmoid(z), h_t = f_t h_{t-1} + (1 - f_t) x_t.
  * z, x, h: rows b*T+t of type T (ld* in elements, >= D, any alignment of an element).  h0 fp32 [B, D], the state that enters
  * step 0 (NULL: zero); hT fp32 [B, D], the state behind the last step (may be NULL).  States are fp32 throughout.  z = +infinity
- * gives f = 1 (the state is kept), -infinity f = 0.  T = 1 is the form for single tokens; h0 and hT may then, as always, be one buffer.
+ * gives f = 1 (the state is kept), -infinity f = 0.  x and h0 are finite: an infinity or NaN among them, or a NaN gate, leaves the state of
+ * its channel infinite or NaN from there on (which of the two is open: steps are composed, and a product of many gates below 1 is 0 in
+ * the end), and of no other.  T = 1 is the form for single tokens; h0 and hT may then, as always, be one buffer.
  * lens: int32 [B], device, or NULL: stream b has lens[b] steps (taken as 0 below 0, as T above T); what the rows behind them
  * hold does not matter, h is zero there, and the state stays what it is.
  * states: fp32 [B, ceil(T / OURO_RECURRENCE_STRIDE), D] or NULL: the state that enters every OURO_RECURRENCE_STRIDE-th
@@ -197,7 +199,8 @@ int ouro_op_recurrence_fwd(void* stream, int dtype, int B, int T, int D, const v
                            const float* h0, const int32_t* lens, void* h, int ldh, float* hT, float* states, float* scratch);
 /* Backward of the above from z, x, states and lens as they were: dh rows of type T, dhT fp32 [B, D] the gradient of hT (NULL:
  * zero).  dz, dx (type T) and dh0 (fp32 [B, D], may be NULL) are overwritten; rows behind a stream's length are zero in dz and dx,
- * and what dh holds there does not matter.  dhT and dh0 may be one buffer. */
+ * and what dh holds there does not matter.  dhT and dh0 may be one buffer.  An infinity or NaN in dh or dhT leaves the gradients of its channel infinite or NaN
+ * from there down to step 0. */
 int ouro_op_recurrence_bwd(void* stream, int dtype, int B, int T, int D, const void* z, int ldz, const void* x, int ldx,
                            const float* states, const int32_t* lens, const void* dh, int lddh, const float* dhT, void* dz,
                            int lddz, void* dx, int lddx, float* dh0, float* scratch);
@@ -233,7 +236,7 @@ int ouro_op_update_tiles(int rows, int cols, int ld_out);
  * whole, the others of the batch are not affected.  The arithmetic is nearly that of fp32 (22-bit operands, fp32
  * sums); entries of X below 2^-37 count as zero, which shows only where eps is many orders above |U|_F.
  * scratch: fp32, ouro_op_orthogonalize_scratch() floats, 16-byte aligned; 0 for sizes that are refused (padded to multiples of 64,
- * rows * cols < 2^29).  What it holds does not matter, so that calls on one stream may share it. */
+ * rows * cols < 2^29 and rows * cols * batch < 2^36; batch <= 65535).  steps: 1 to 100.  What it holds does not matter, so that calls on one stream may share it. */
 int ouro_op_orthogonalize(void* stream, int dtype, int batch, int rows, int cols, const void* g, int ldg, long long sg, float* momentum, float mu,
                           int nesterov, void* o, int ldo, long long so, float scale, float eps, int steps, float* scratch);
 size_t ouro_op_orthogonalize_scratch(int batch, int rows, int cols);

@@ -420,3 +420,40 @@ def test_a_kept_state_on_the_device(B, T, D, dtype):
     for k in ("dz", "dx"):
         assert not s["out"][k][:, lo:hi].any(), k
         assert s["out"][k][:, :lo].any() and s["out"][k][:, hi:].any(), k
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("B,T,D", [(2, 900, 24), (520, 600, 8)])
+def test_an_infinity_stays_in_its_channel(B, T, D, dtype):
+    """In x, h0, dh or dhT: not finite behind it (its gradients: before it), everything else as without it, bit for bit."""
+    s = make(B, T, D, dtype, T)
+    forward(s)
+    backward(s)
+    clean = {k: v.clone() for k, v in (*s["out"].items(), ("hT", s["hT"]), ("dh0", s["dh0"]))}
+    at = T // 2
+
+    def same_but(name, got, bad):
+        assert not torch.isfinite(got[bad]).any(), name
+        got = got.clone()
+        got[bad] = clean[name][bad]
+        assert torch.equal(got, clean[name]), name
+
+    for value in (float("inf"), float("-inf")):
+        kept = s["x"][1, at, 5].clone(), s["h0"][0, 3].clone()
+        s["x"][1, at, 5] = s["h0"][0, 3] = value
+        forward(s)
+        bad = torch.zeros(B, T, D, dtype=torch.bool, device="cuda")
+        bad[1, at:, 5] = bad[0, :, 3] = True
+        same_but("h", s["out"]["h"], bad)
+        same_but("hT", s["hT"], bad[:, -1])
+        s["x"][1, at, 5], s["h0"][0, 3] = kept
+        forward(s)
+        kept = s["dh"][1, at, 5].clone(), s["dhT"][0, 3].clone()
+        s["dh"][1, at, 5] = s["dhT"][0, 3] = value
+        backward(s)
+        bad = torch.zeros(B, T, D, dtype=torch.bool, device="cuda")
+        bad[1, :at + 1, 5] = bad[0, :, 3] = True
+        for k in ("dz", "dx"):
+            same_but(k, s["out"][k], bad)
+        same_but("dh0", s["dh0"], bad[:, 0])
+        s["dh"][1, at, 5], s["dhT"][0, 3] = kept
