@@ -195,7 +195,8 @@ hipError_t launch_attn_bwd(hipStream_t s, int dtype, const AttnDesc& a, int forc
 
 // --------------------------------------------------------------------------- recurrence
 // h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(z), per stream and channel; rows b*T + t of type T, states fp32 [B, D].
-// Steps t >= lens[b] (null: none) are not taken, their rows not read and written as zero.  states [B, ceil(T / stride), D]: the
+// Steps t >= lens[b] (null: none) are not taken: whatever their rows hold does not matter (they are read along), and those of the
+// results are written as zero.  states [B, ceil(T / stride), D]: the
 // state that enters every RECURRENCE_STRIDE-th step (forward: written unless null; backward: read).  dz null: forward.
 constexpr int RECURRENCE_STRIDE = 64;
 struct RecurrenceDesc {

@@ -5,7 +5,8 @@
 // columns of dh.  It reads all N ids (they stay in L2), keeps those of its rows as a list in LDS, sorts the list by row with a
 // stable sort, and its teams of 8 lanes (16 bytes each) sum equal pieces of the sorted list: a frequent token is summed by
 // many teams, whose parts are joined in order through LDS; one of thousands of ids is summed without a list.  Every sum therefore
-// has an order that only the ids determine.  Rows are dealt to workgroups by v mod R because ids are usually ranked by frequency:
+// has an order that only the ids determine.  Ids that a list or an entry's position has no room for are summed after those before them, onto
+// what the matrix then holds.  Rows are dealt to workgroups by v mod R because ids are usually ranked by frequency:
 // neighbours are alike in weight.
 //
 // Bound by memory: N d elements read, the matrix written (or the rows of tokens that occur read and written).  8192 ids, 32768 x 512 in
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(ES_THREADS, 4) void embed_bwd_sorted_kernel(EmbedSo
   const int team = tid / STRIP_LANES;
   for (int i = tid; i < 1 << max(0, p.row_bits - 5); i += ES_THREADS) seen[i] = 0;
 
-  // ---- a token of very many ids: no list holds them, and its rows come in any order
+  // ---- a token of very many ids, which no list holds: its rows are summed in the order of the ids in a team, as they are found
   const int hot = p.N > 4 * ES_HOT ? es_hot(p, R, mine) : -1;
   if (hot >= 0) {
     float* heads = reinterpret_cast<float*>(hist_or_heads);

@@ -1,12 +1,14 @@
 // Orthogonalised updates: X = U / (|U|_F + eps), then steps of X <- a X + (b A + c A^2) X with A = X X^T, which drive the singular
-// values of U towards 1 and leave its singular vectors (Newton-Schulz with the quintic whose coefficients are below).  U is the
-// gradient or its momentum.
+// values of U towards 1 and leave its singular vectors (Newton-Schulz with the quintic whose coefficients are below, which Jordan et al.
+// published for orthogonalised momentum in 2024).  U is the gradient or its momentum.
 //
 // The products run on fp16 matrix instructions with every operand as a sum of two fp16 numbers, high + low (22 bits of
 // mantissa): x y = xh yh + xh yl + xl yh with fp32 accumulation.  One fp16 (or bf16) number is not enough: a step multiplies small singular
 // values by a, five steps by 485, and with them the rounding noise of X: with 16 strong directions over noise of 1e-4 one
 // fp16 number gives an error of 4.5e-2, bf16 0.37, the two halves 8e-6 and fp32 arithmetic 5e-6 (random matrices: 1.4e-3, 1.1e-2,
-// 2.6e-7, 1.7e-7).  All entries of X, A and the polynomials are below 12 in magnitude (|X|_2 <= 1.2, |C|_2 <= 3.5); they are stored times 2^12, so that
+// 2.6e-7, 1.7e-7).  On the device, against fp32 products of the library: 0.6 to 0.9 times their error where the matrix is a few hundred wide, 1.5 times at
+// 1024 x 4096 (6.3e-6 against 4.1e-6).  The fourth product, low x low, would cost a third more; it is at most 2^-22 of the whole, as much as rounding the low
+// halves costs.  All entries of X, A and the polynomials are below 12 in magnitude (|X|_2 <= 1.2, |C|_2 <= 3.5); they are stored times 2^12, so that
 // the low halves of ordinary entries (1 / sqrt(rows cols)) stay above fp16's smallest normal number.
 //
 // With C = a I + b A + c A^2 a step is X <- C X, and the A of the step after it is C A C: all of these are polynomials of one symmetric
@@ -15,8 +17,10 @@
 // 2.0 -> 1.4 ms).  It is as accurate: errors of A' are absolute, 2^-22 |A|, and reach X through C' as 1e-6 of a.  Three steps without X
 // would not be: negative rounding noise in the small eigenvalues of A grows by a^2 a step.
 //
-// Bound by the matrix instructions where matrices are large: 24 of 1024 x 4096, five steps, 3.72 ms, three times 1.21 TFLOP at 0.98 PFLOP/s (a large
-// fp16 product reaches 1.02); by the latency of 17 dependent products where they are small (four of 2100 x 410: 222 us).
+// Bound by the matrix instructions where matrices are large: 24 of 1024 x 4096, five steps, 3.75 ms, three times 1.21 TFLOP at 0.97 PFLOP/s.  A
+// library product of 8192^3 reaches 1.54 in fp16 (1.62 in bf16, this main loop with bf16 operands 1.45).  The products with X run at 1.13 of that; the
+// symmetric ones at 0.76, counting half of each: 10 whole 256 wide tiles hold the 8 that are needed, 240 of them for 256 CUs.  Bound by the latency of 17 dependent
+// products where matrices are small (four of 2100 x 410: 221 us).
 //
 // All products are of the form L R^T with the contraction contiguous in both: X X^T; products of two of the symmetric matrices; and one of
 // those times X^T, for which X is kept in both layouts.  Of the symmetric results only the tiles on and below the diagonal are formed, and
@@ -344,7 +348,8 @@ __device__ __forceinline__ void ns_request(const char* base, int bytes, char* ds
 }
 
 // 64 S x 64 S tiles, four waves of 32 S x 32 S each.  A K-tile is 32 of the contraction: 128-byte rows of high and low halves in LDS, 16-byte
-// chunk c of a row at c ^ swizzle(row), in a ring of D stages filled by direct loads that stay in flight over the barriers.  G groups
+// chunk c of a row at c ^ swizzle(row), in two stages filled by direct loads: a K-tile's are requested when the one before it has arrived, and are waited
+// for, all of them, before the barrier that opens it.  G groups
 // of four waves take every G-th K-tile each and are added up in order at the end: with one workgroup a CU a K-tile costs its latency
 // (wait, barrier, fragments, six dependent matrix instructions: 0.37 us), and four at a time a quarter of it.
 template <int S, int G> struct NsSmall {

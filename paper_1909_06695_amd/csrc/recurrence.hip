@@ -5,7 +5,8 @@
 // scan over these, and with the state that enters its steps known each thread runs them once more from registers.
 // Backward, with G_t = dh_t + f_{t+1} G_{t+1} and P_t = f_t G_t: P_t = f_t P_{t+1} + f_t dh_t, the same kind of map from the right with the
 // same factors; dx_t = (1 - f_t) G_t, dz_t = G_t (h_{t-1} - x_t) f_t (1 - f_t).  h is formed again from the fp32 states that the forward
-// pass left at every 64th step, so that it is neither read back nor rounded.
+// pass left at every 64th step, so that it is neither read back nor rounded.  (Recurrences as scans over maps that compose: Blelloch 1990; tiles that publish
+// their map, then the state behind them, and look back over those before: Merrill and Garland 2016.)
 //
 // Bound by memory: z, x (and dh) read once, h (or dz, dx) written once.  A workgroup owns 128 bytes of channels of one stream and a
 // tile of steps (256 in bf16, 512 in fp32, backward half of that).  Where streams and channels fill the chip it walks over its tiles itself.  Where they do not,
@@ -13,7 +14,8 @@
 // before these, and publishes the state behind itself.  The tiles of a line (a strip of a stream) are dealt by a counter, so that a
 // workgroup only waits for workgroups that have begun before it and every wait ends.  Nothing is read twice.
 // 8 streams of 1024 steps, 1024 channels, bf16: forward 16 us (51 MB, 3.2 TB/s), backward 25 us (84 MB, 3.4 TB/s), 2 and 4 of them for clearing the
-// workspace; one of 65536 steps, 512 channels, fp32: forward 91 us (405 MB, 4.5 TB/s); 64 single tokens of 1024 channels: 5 us.
+// workspace; one of 65536 steps, 512 channels, fp32: forward 91 us (405 MB, 4.5 TB/s); 64 single tokens of 1024 channels: 5 us.  32 streams of 1024 steps,
+// 1024 channels, bf16, which a workgroup walks over: 36 us (201 MB, 5.6 TB/s: repeated calls find part of it in the memory-side cache) and 92 us (336 MB, 3.7 TB/s).
 #include "common.h"
 #include "unaligned.h"
 
@@ -422,7 +424,11 @@ __global__ __launch_bounds__(64 * RC_WAVES, 4) void recurrence_bwd_kernel(Recurr
   if (nth == p.tiles && a.wave == 0 && c.on && p.dh0) p.dh0[c.state] = carry;
 }
 
-// How a call is laid out: a workgroup a tile where strips and streams alone are fewer workgroups than the chip holds (two a CU).
+// How a call is laid out: a workgroup a tile where strips and streams alone are fewer workgroups than the chip holds (two a CU).  There walking
+// over the tiles needs no workspace and is as fast or faster forward (chained against walking, bf16, 1024 steps and channels: 128 lines 15.7 against
+// 20.1 us, 256 lines 26.6 / 23.9, 512 42.8 / 36.1, 1024 94.4 / 93.7; fp32: 256 lines 20.5 / 21.0, 512 37.0 / 32.3), but where streams are long (8192 steps, fp32, 512
+// lines: 306 against 364).  Backward it is behind: bf16, 128 lines 26 against 43 us, 256 40 / 46, 512 85 / 92, 768 122 / 156, 1024
+// 157 / 173 (512 lines of 300 steps: 31 / 29); fp32, 512 lines 90 / 98.  There the rule buys little but the workspace.
 struct RcPlan { int strips, waves, tiles, mode; };
 static RcPlan rc_plan(int dtype, bool backward, int B, int T, int D) {
   RcPlan r;
