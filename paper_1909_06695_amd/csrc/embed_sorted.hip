@@ -14,6 +14,7 @@
 // that own its row, at about 12 bytes/ns each (the lines a CU has under way): 8192 ids, a quarter of them one token, added to 50257 x
 // 1024: 25 us (50 MB), 9 of which go to finding and sorting the entries.  Without a workspace no others can share them.
 #include "common.h"
+#include "embed_sample.h"
 #include "unaligned.h"
 
 #include <algorithm>
@@ -103,7 +104,7 @@ __device__ __forceinline__ void es_clear(const EmbedSortedParams& p, uint32_t z0
 
 // A token of the workgroup's rows that makes up ES_HOT ids and more by a sample of 64 of them, or -1 (every wave finds the same).
 __device__ __forceinline__ int es_hot(const EmbedSortedParams& p, uint32_t R, uint32_t mine) {
-  const int lane = threadIdx.x & 63, id = p.tok[(long)lane * p.N / 64];
+  const int lane = threadIdx.x & 63, id = p.tok[es_sample_at(lane, p.N)];
   const bool on = (uint32_t)id < (uint32_t)p.vocab && ((uint32_t)id & (R - 1)) == mine;
   uint32_t best = (uint32_t)__popcll(es_peers((uint32_t)id, 31, __ballot(on))) << 6 | (uint32_t)lane;
   if (!on) best = 0;

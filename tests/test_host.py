@@ -316,3 +316,28 @@ def test_bytes_of_a_timed_update(fake_hip):
 
 def test_recurrences_of_any_length_can_be_launched(fake_hip):
     fake_hip("recurrences_of_any_length")
+
+
+def test_the_sample_of_ids_is_at_every_place_of_a_stream(tmp_path):
+    """64 of N ids, from which the sorted embedding gradient tells whether one token makes up most of them: in order, within N, and whatever the length of the
+    streams that N is cut into, no more than 1 in 8 of them at the streams' first ids, and as large a share behind 2/5 and 3/4 of a stream as there are ids, to
+    0.15 (a sample at equal distances has 1 or 0 where the streams divide these)."""
+    src = tmp_path / "sample.cpp"
+    src.write_text('#include "embed_sample.h"\nextern "C" int at(int lane, int n) { return ouro::es_sample_at(lane, n); }\n')
+    so = str(tmp_path / "sample.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_1909_06695_amd", "csrc"), "-o", so, str(src)], check=True)
+    import ctypes
+    at = ctypes.CDLL(so).at
+    for S in (16, 50, 64, 100, 128, 150, 256, 384, 500, 512, 777, 1024, 2048, 4096):
+        for streams in (8, 16, 31, 32, 64, 100, 128, 256, 512):
+            N = S * streams
+            if not 16384 < N <= 1 << 20:
+                continue
+            places = [at(lane, N) for lane in range(64)]
+            assert places == sorted(places) and 0 <= places[0] and places[-1] < N
+            within = [p % S for p in places]
+            assert within.count(0) <= 8, (S, streams)
+            for part in (0.4, 0.75):
+                share = sum(w >= part * S for w in within) / 64
+                assert abs(share - (1 - part)) <= 0.15, (S, streams, part, share)
+    assert at(63, 1 << 30) < 1 << 30
