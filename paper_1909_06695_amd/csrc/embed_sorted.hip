@@ -12,7 +12,7 @@
 // Bound by memory: N d elements read, the matrix written (or the rows of tokens that occur read and written).  8192 ids, 32768 x 512 in
 // fp32: 21 us (84 MB, 4.0 TB/s); 4800 ids, 32768 x 410 in bf16: 23 us (58 MB).  Where one token makes up much of the ids, by the workgroups
 // that own its row, at about 12 bytes/ns each (the lines a CU has under way): 8192 ids, a quarter of them one token, added to 50257 x
-// 1024: 25 us (50 MB), 9 of which go to finding and sorting the entries.  Without a workspace no others can share them.
+// 1024: 24 to 28 us with the ids (50 MB), 9 of which go to finding and sorting the entries.  Without a workspace no others can share them.
 #include "common.h"
 #include "embed_sample.h"
 #include "unaligned.h"
